@@ -17,7 +17,9 @@
  *   only memory the library allocates itself is a set of workspaces, one of
  *   each kind per (device, stream): the split-tile partials of ue5m3_gemm,
  *   the expanded block-32 scales of ue5m3_gemm_ex / ue5m3_gemm_pm, and
- *   16 KiB of per-workgroup partial maxima for the amax calls.  A workspace
+ *   16 KiB of per-workgroup partial maxima for the amax calls, the column
+ *   sums of ue5m3_layer_norm_grad and the quantized tokens of
+ *   ue5m3_linear_fp8.  A workspace
  *   is allocated (hipMalloc) by the first call on that pair that needs it,
  *   or needs a larger one; a replaced workspace is never freed before the
  *   process ends, so work already enqueued or captured in a graph keeps a
@@ -104,7 +106,10 @@ typedef enum {
     UE5M3_TILE16 = 2,
     UE5M3_ROW32 = 3,
     UE5M3_COL32T = 4,
-    UE5M3_TILE32 = 5
+    UE5M3_TILE32 = 5,
+    UE5M3_ROW128 = 6,   /* the 8-bit formats' blocks and tiles of 128: */
+    UE5M3_COL128T = 7,  /* ue5m3_gemm_fp8 only                         */
+    UE5M3_TILE128 = 8
 } ue5m3_blocking_t;
 
 /*
@@ -474,6 +479,133 @@ ue5m3_status_t ue5m3_gemm_pm(ue5m3_layout_t layout, int64_t M, int64_t N, int64_
                              ue5m3_blocking_t b_blk, const float* b_dec, void* c,
                              ue5m3_out_t c_type, ue5m3_scale_kind_t scale_kind,
                              int32_t grid_d, hipStream_t stream);
+
+/*
+ * ------------------------------------------------------------------------
+ * Operators around the linear layers: layer norm, a linear layer's products in
+ * 8-bit floating point, dropout.  The conventions at the top of this file
+ * hold, with these differences: bare tensors (x, dy, weight, bias, residual
+ * and their outputs) need the alignment of their element only, and any
+ * size, odd ones included; payloads, scales and GEMM outputs are 16-byte
+ * aligned.  Outputs do not overlap inputs unless stated.
+ * ------------------------------------------------------------------------
+ */
+
+/* Element types. */
+typedef enum { UE5M3_BF16 = 0, UE5M3_F16 = 1, UE5M3_F32 = 2 } ue5m3_dtype_t;
+
+/* OCP 8-bit formats: E4M3 (bias 7, largest 448, no infinities) and E5M2
+ * (bias 15, largest finite 57344). */
+typedef enum { UE5M3_E4M3 = 0, UE5M3_E5M2 = 1 } ue5m3_fp8_t;
+
+/* Block scales of the 8-bit operands: binary32 numbers, or powers of two as
+ * E8M0 bytes (value 2^(code - 127)), which the matrix instructions apply
+ * themselves. */
+typedef enum { UE5M3_FP8_SCALE_F32 = 0, UE5M3_FP8_SCALE_E8M0 = 1 } ue5m3_fp8_scale_t;
+
+/*
+ * Layer norm of x [rows, cols] (dense, x_type) over its rows:
+ *     mean = sum(x) / cols, rstd = 1 / sqrt(sum((x - mean)^2) / cols + eps),
+ *     y = (x - mean) rstd weight + bias,
+ * in binary32, y rounded once to x_type.  weight and bias [cols] (nullable: 1
+ * and 0) have param_type, which is x_type or UE5M3_F32.  mean and rstd
+ * (nullable) receive the rows' statistics, for ue5m3_layer_norm_grad.
+ * EINVAL: a bad type, eps negative or not finite, a null x or y; ESHAPE: a
+ * negative size, or cols >= 2^31; EALIGN.  rows = 0 or cols = 0 does
+ * nothing.
+ */
+ue5m3_status_t ue5m3_layer_norm(const void* x, int64_t rows, int64_t cols, ue5m3_dtype_t x_type, const void* weight,
+                                const void* bias, ue5m3_dtype_t param_type, float eps, void* y, float* mean,
+                                float* rstd, hipStream_t stream);
+
+/*
+ * The gradients of ue5m3_layer_norm for the output gradient dy (x_type):
+ * with h = (x - mean) rstd and g = dy weight,
+ *     dx = rstd (g - sum(g) / cols - h sum(g h) / cols) [+ residual_grad],
+ *     dweight = sum over rows of dy h, dbias = sum over rows of dy,
+ * in binary32, rounded once (dx to x_type, dweight and dbias to param_type).
+ * Each output is nullable; residual_grad (nullable, [rows, cols] of x_type) is
+ * the gradient that reaches x past the norm.  The column sums are added in a
+ * fixed order: the same call gives the same bits.  They pass through a library
+ * workspace (see the conventions).  rows = 0 writes zeros to dweight and dbias.
+ */
+ue5m3_status_t ue5m3_layer_norm_grad(const void* x, const void* dy, int64_t rows, int64_t cols, ue5m3_dtype_t x_type,
+                                     const void* weight, ue5m3_dtype_t param_type, const float* mean,
+                                     const float* rstd, const void* residual_grad, void* dx, void* dweight,
+                                     void* dbias, hipStream_t stream);
+
+/*
+ * Dropout of n elements: y_i = [residual_i +] (keep_i ? x_i s : 0), in
+ * binary32, rounded once; residual is nullable and y may be x or residual.
+ * keep_i = (w_i >= d) with d = round(65536 p) (ties to even), s = 65536 / (65536 - d)
+ * (0 for d = 65536) and w_i the 16 bits 16 (i % 2) .. +15 of word (i % 8) / 2
+ * of Philox4x32-10 with key (seed lo, seed hi) and counter (i / 8 as 64 bits,
+ * tensor_id, 1).  The same call on the output gradient, without residual, is
+ * the backward pass: no mask is stored.  EINVAL: p outside [0, 1], a bad type,
+ * a null x or y with n > 0; ESHAPE: n < 0; EALIGN.
+ */
+ue5m3_status_t ue5m3_dropout(const void* x, int64_t n, ue5m3_dtype_t type, double p, uint64_t seed,
+                             uint32_t tensor_id, const void* residual, void* y, hipStream_t stream);
+
+/*
+ * Quantizes x [rows, cols] (dense, x_type) to 8-bit floating point in blocks
+ * of 128: along its rows (payload_r, scales_r), down its columns (payload_c,
+ * scales_c), or both from one read; a pair that is not wanted is null, null.
+ * With a the largest finite magnitude of a block and F the format's largest
+ * value:
+ *   UE5M3_FP8_SCALE_F32   a' = max(a, F 2^-126); scale a' / F; element x F / a'
+ *   UE5M3_FP8_SCALE_E8M0  scale 2^e, e >= -126 the least with a <= F 2^e;
+ *                         element x 2^-e
+ * (a = 0: scale 1), rounded to the nearest value of the format, ties to even.
+ * An infinity or a NaN becomes a NaN of the format.  Layouts, with
+ * pad(n) = n rounded up to a multiple of 128 and pitch(n) to one of 16:
+ *   payload_r [rows][pad(cols)], scales_r [pad(cols) / 128][pitch(rows)],
+ *   payload_c [cols][pad(rows)], scales_c [pad(rows) / 128][pitch(cols)]
+ * (transposed, as the row blocking of x^T).  Bytes past a row's end are
+ * written as zeros, scales past the last row are not written.  The last block
+ * of a row is short when the size is no multiple of 128.
+ */
+ue5m3_status_t ue5m3_quantize_fp8(const void* x, int64_t rows, int64_t cols, ue5m3_dtype_t x_type, ue5m3_fp8_t format,
+                                  ue5m3_fp8_scale_t scale_kind, uint8_t* payload_r, void* scales_r,
+                                  uint8_t* payload_c, void* scales_c, hipStream_t stream);
+
+/*
+ * The same in tiles of 128 x 128, to E4M3 (weights: the row and the column
+ * view of a product share the values):
+ *   payload   [rows][pad(cols)], scales   [pad(rows) / 128][pad(cols) / 128]
+ *   payload_t [cols][pad(rows)], scales_t [pad(cols) / 128][pad(rows) / 128]
+ * (both nullable together): the transposed copy.
+ */
+ue5m3_status_t ue5m3_quantize_fp8_tiles(const void* w, int64_t rows, int64_t cols, ue5m3_dtype_t w_type,
+                                        ue5m3_fp8_scale_t scale_kind, uint8_t* payload, void* scales,
+                                        uint8_t* payload_t, void* scales_t, hipStream_t stream);
+
+/*
+ * C[m, n] = sum over blocks of 128 k of (scale_a scale_b sum over the block of
+ * a b): products of 8-bit values are exact, sums in binary32 in an unspecified
+ * order; C as for ue5m3_gemm.  Operands as the two calls above write them:
+ * A (a_format) blocked by UE5M3_ROW128 or UE5M3_COL128T, B (E4M3) by those or
+ * UE5M3_TILE128, with the layouts and the blocking rule of ue5m3_gemm (NT: A
+ * ROW128, B ROW128 or TILE128; NN: A ROW128, B COL128T or TILE128, its
+ * transposed copy; TN: A COL128T, B COL128T or TILE128, transposed); other
+ * blockings are UE5M3_ELAYOUT, unknown ones and those of 16 and 32 UE5M3_EINVAL.
+ * scale_kind holds for both operands.  Any M, N, K >= 0 (K <= 2^22); M = 0 or
+ * N = 0 writes nothing, K = 0 zeros.
+ */
+ue5m3_status_t ue5m3_gemm_fp8(ue5m3_layout_t layout, int64_t M, int64_t N, int64_t K, const uint8_t* a,
+                              const void* a_scales, ue5m3_blocking_t a_blk, ue5m3_fp8_t a_format, const uint8_t* b,
+                              const void* b_scales, ue5m3_blocking_t b_blk, ue5m3_fp8_scale_t scale_kind, void* c,
+                              ue5m3_out_t c_type, hipStream_t stream);
+
+/*
+ * A serving call of a linear layer: y [T, N] = x [T, K] W^T for bf16 tokens x
+ * and a weight quantized once by ue5m3_quantize_fp8_tiles (w, w_scales).  The
+ * tokens are quantized along their rows (E4M3, scale_kind) and multiplied, with
+ * the result of the two calls; what is between them is in a library workspace.
+ */
+ue5m3_status_t ue5m3_linear_fp8(const void* x_bf16, int64_t T, int64_t K, int64_t N, const uint8_t* w,
+                                const void* w_scales, ue5m3_fp8_scale_t scale_kind, void* y, ue5m3_out_t y_type,
+                                hipStream_t stream);
 
 /* Static description of a status code. */
 const char* ue5m3_status_string(ue5m3_status_t status);

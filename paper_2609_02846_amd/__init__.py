@@ -37,6 +37,8 @@ EXPORTED_SYMBOLS = (
     "ue5m3_quantize_1d_ex", "ue5m3_quantize_2d_ex", "ue5m3_gemm_ex", "ue5m3_quantize_dual",
     "ue5m3_gemm_pm", "ue5m3_amax_sample_rht", "ue5m3_quantize_cols_rht",
     "ue5m3_status_string", "ue5m3_version", "ue5m3_gemm_noalloc",
+    "ue5m3_layer_norm", "ue5m3_layer_norm_grad", "ue5m3_dropout",
+    "ue5m3_quantize_fp8", "ue5m3_quantize_fp8_tiles", "ue5m3_gemm_fp8", "ue5m3_linear_fp8",
 )
 
 
@@ -104,6 +106,21 @@ def load_library(path=LIB_PATH):
     lib.ue5m3_quantize_dual.argtypes = [vp, i64, i64, vp, f32, i32, u64, u32, u32, i32,
                                         vp, vp, vp, vp, vp, vp]
     lib.ue5m3_quantize_dual.restype = i32
+    f64 = ctypes.c_double
+    lib.ue5m3_layer_norm.argtypes = [vp, i64, i64, i32, vp, vp, i32, f32, vp, vp, vp, vp]
+    lib.ue5m3_layer_norm.restype = i32
+    lib.ue5m3_layer_norm_grad.argtypes = [vp, vp, i64, i64, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.ue5m3_layer_norm_grad.restype = i32
+    lib.ue5m3_dropout.argtypes = [vp, i64, i32, f64, u64, u32, vp, vp, vp]
+    lib.ue5m3_dropout.restype = i32
+    lib.ue5m3_quantize_fp8.argtypes = [vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.ue5m3_quantize_fp8.restype = i32
+    lib.ue5m3_quantize_fp8_tiles.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp, vp, vp]
+    lib.ue5m3_quantize_fp8_tiles.restype = i32
+    lib.ue5m3_gemm_fp8.argtypes = [i32, i64, i64, i64, vp, vp, i32, i32, vp, vp, i32, i32, vp, i32, vp]
+    lib.ue5m3_gemm_fp8.restype = i32
+    lib.ue5m3_linear_fp8.argtypes = [vp, i64, i64, i64, vp, vp, i32, vp, i32, vp]
+    lib.ue5m3_linear_fp8.restype = i32
     lib.ue5m3_status_string.argtypes = [i32]
     lib.ue5m3_status_string.restype = ctypes.c_char_p
     lib.ue5m3_version.argtypes = []
@@ -450,3 +467,7 @@ def gemm_noalloc(layout, M, N, K, a, a_scales, a_dec, b, b_scales, b_dec, out, s
                            a_blk, b_blk)
     _check(load_library().ue5m3_gemm_noalloc(*args, _stream(stream)), "ue5m3_gemm_noalloc")
     return out
+
+
+from .operators import (dropout_forward, gemm_fp8, layer_norm_forward, layer_norm_grad, linear_fp8,  # noqa: E402
+                        quantize_fp8, quantize_fp8_dual, quantize_fp8_tiles)

@@ -17,12 +17,18 @@ enum class BScale : int { Row = 0, Tile = 1, TileDgrad = 2 };
 // NVFP4-style) or E8M0 (blocks of 32, MXFP4-style, no tensor scale).
 enum class ScaleKind : int { UE5M3 = 0, E4M3 = 1, E8M0 = 2 };
 
+// Element type of the operators around the linear layers (layer norm, dropout,
+// the 8-bit quantizers), and the 8-bit formats.
+enum class DType : int { BF16 = 0, F16 = 1, F32 = 2 };
+enum class Fp8 : int { E4M3 = 0, E5M2 = 1 };
+
 // Library workspaces, one per (kind, device, stream), allocated on first
 // need and replaced by a larger one on demand (the replaced buffer is kept,
 // not freed, until the process ends): split-tile partials of the GEMMs,
 // block-32 scales expanded to the block-16 layout, per-workgroup partial
-// maxima of the amax kernels.
-enum WorkspaceKind : int { kWsSplit = 0, kWsScales = 1, kWsAmax = 2, kWsKinds = 3 };
+// maxima of the amax kernels, per-workgroup column sums of layer norm's
+// backward pass, the quantized tokens of a serving call.
+enum WorkspaceKind : int { kWsSplit = 0, kWsScales = 1, kWsAmax = 2, kWsNorm = 3, kWsTokens = 4, kWsKinds = 5 };
 
 // One call's use of a workspace.  Uses on one stream are ordered by the
 // stream as long as each call's launches are enqueued together, so the
@@ -153,5 +159,40 @@ hipError_t launch_gemm_b32(BScale bmode, float amul, bool pm, float grid_d, int6
 hipError_t launch_gemm_mx(int64_t M, int64_t N, int64_t K, const uint8_t* a, const uint8_t* a_scales,
                           const float* a_dec, const uint8_t* b, const uint8_t* b_scales,
                           const float* b_dec, void* c, bool c_bf16, hipStream_t s);
+
+// Layer norm over rows of C elements; w, b, mean and rstd may be null.
+hipError_t launch_norm(DType type, const void* x, int64_t rows, int64_t C, DType ptype, const void* w, const void* b,
+                       float eps, void* y, float* mean, float* rstd, hipStream_t s);
+
+// Its gradients; w, res, dx, dw and db may be null.  The column sums' partials
+// go through a workspace.
+hipError_t launch_norm_grad(DType type, const void* x, const void* dy, int64_t rows, int64_t C, DType ptype,
+                            const void* w, const float* mean, const float* rstd, const void* res, void* dx, void* dw,
+                            void* db, hipStream_t s);
+
+// y = [residual +] dropout(x) over n elements; residual may be null, y may be x.
+hipError_t launch_dropout(DType type, const void* x, int64_t n, double p, uint64_t seed, uint32_t tensor_id,
+                          const void* residual, void* y, hipStream_t s);
+
+// Quantizers in blocks of 128 along the rows (rows, rows_scale) and down the
+// columns (cols, cols_scale), either pair or both; e8: E8M0 scale codes, else
+// binary32 scales.
+hipError_t launch_quant_fp8(DType type, Fp8 fmt, bool e8, const void* x, int64_t R, int64_t C, uint8_t* rows,
+                            void* rows_scale, uint8_t* cols, void* cols_scale, hipStream_t s);
+
+// Quantizer in tiles of 128 x 128 (E4M3), with the transposed copy unless
+// payload_t is null.
+hipError_t launch_quant_fp8_tiles(DType type, bool e8, const void* w, int64_t R, int64_t C, uint8_t* payload,
+                                  void* scales, uint8_t* payload_t, void* scales_t, hipStream_t s);
+
+// C [M, N] from operands in blocks of 128 along K; tiled: one B scale for 128
+// rows; B is E4M3.
+hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
+                           const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16, hipStream_t s);
+
+// y [T, N] = x [T, K] times a weight in tiles, transposed: quantizes x to a
+// workspace, then the product.
+hipError_t launch_linear_fp8(const void* x_bf16, int64_t T, int64_t K, int64_t N, const uint8_t* w, const void* ws,
+                             bool e8, void* y, bool y_bf16, hipStream_t s);
 
 }  // namespace ue5m3

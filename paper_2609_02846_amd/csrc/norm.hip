@@ -1,0 +1,446 @@
+// Layer norm over rows of C elements, forward and backward.
+//
+//   mean = sum(x) / C, rstd = 1 / sqrt(sum((x - mean)^2) / C + eps),
+//   h = (x - mean) rstd, y = h w + b
+//   g = dy w, dx = rstd (g - sum(g) / C - h sum(g h) / C) [+ the residual's
+//   gradient], dw = sum over rows of dy h, db = sum over rows of dy
+//
+// All in binary32; x, dy and the outputs are read and written once, rounded
+// once.  A row stays in the registers of NW waves (U vectors of eight elements
+// a lane), so the variance is the sum of squared distances from the mean that
+// is already known, and the backward pass reads each tensor once.
+//
+// Bound: HBM.  The backward pass's column sums stay in registers too, over all
+// the rows that a workgroup takes; each workgroup then writes one row of
+// partial sums, and a second kernel adds those rows in order, so the result
+// does not depend on which workgroup ended first.
+#include "io.hpp"
+
+namespace ue5m3 {
+namespace {
+
+constexpr int kBwdThreads = 1024;
+
+// Sum of v over the NW waves that share a row, in each of their lanes.  `red`
+// holds one float for each wave of the workgroup; the caller alternates two
+// of them, so that one barrier a sum is enough: a slot is written again only
+// after the next sum's barrier.
+template <int NW>
+__device__ __forceinline__ float row_sum(float v, float* red, int wave) {
+    v = wave_sum(v);
+    if (NW == 1) return v;
+    if ((threadIdx.x & 63) == 0) red[wave] = v;
+    __syncthreads();
+    const int first = wave / NW * NW;
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) s += red[first + k];
+    return s;
+}
+
+template <typename T, typename P, int NW, int U>
+__global__ __launch_bounds__(NW > 4 ? 64 * NW : 256) void norm_fwd_kernel(const T* __restrict__ x,
+                                                                          const P* __restrict__ w,
+                                                                          const P* __restrict__ b, T* __restrict__ y,
+                                                                          float* __restrict__ mean_out,
+                                                                          float* __restrict__ rstd_out, int64_t rows,
+                                                                          int C, float eps) {
+    constexpr int kThreads = NW > 4 ? 64 * NW : 256, kRows = kThreads / 64 / NW;
+    __shared__ float red[2][kThreads / 64];
+    const int wave = threadIdx.x >> 6, c0 = ((wave % NW) * 64 + (threadIdx.x & 63)) * 8;
+    const float inv = 1.0f / (float)C;
+    // a workgroup's waves take the same number of turns (they share barriers)
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < rows; r0 += (int64_t)gridDim.x * kRows) {
+        const int64_t r = r0 + wave / NW;
+        const bool live = r < rows;
+        const T* xr = x + r * C;
+        Vec8<T> v[U];
+        float sum = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            v[u] = load8(xr, c0 + u * NW * 512, live ? C : 0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += (float)v[u].e[e];
+        }
+        const float mean = row_sum<NW>(sum, red[0], wave) * inv;
+        float sq = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = (float)v[u].e[e] - mean;
+                sq += c0 + u * NW * 512 + e < C ? d * d : 0.0f;
+            }
+        const float rstd = 1.0f / sqrtf(row_sum<NW>(sq, red[1], wave) * inv + eps);
+        if (!live) continue;
+        if (c0 == 0) {
+            if (mean_out != nullptr) mean_out[r] = mean;
+            if (rstd_out != nullptr) rstd_out[r] = rstd;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * NW * 512;
+            if (c >= C) break;
+            Vec8<P> wv, bv;
+            if (w != nullptr) wv = load8(w, c, C);
+            if (b != nullptr) bv = load8(b, c, C);
+            Vec8<T> o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float h = ((float)v[u].e[e] - mean) * rstd;
+                if (w != nullptr) h *= (float)wv.e[e];
+                if (b != nullptr) h += (float)bv.e[e];
+                o.e[e] = (T)h;
+            }
+            store8(y + r * C, c, C, o);
+        }
+    }
+}
+
+// Rows too long for the registers: one workgroup a row, which it reads three
+// times (the second and third time from the caches).
+template <typename T, typename P>
+__global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const T* __restrict__ x, const P* __restrict__ w,
+                                                             const P* __restrict__ b, T* __restrict__ y,
+                                                             float* __restrict__ mean_out, float* __restrict__ rstd_out,
+                                                             int64_t rows, int64_t C, float eps) {
+    __shared__ float red[2][16];
+    const int wave = threadIdx.x >> 6;
+    const float inv = 1.0f / (float)C;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const T* xr = x + r * C;
+        float sum = 0.0f;
+        for (int64_t c = 8 * (int64_t)threadIdx.x; c < C; c += 8192) {
+            const Vec8<T> v = load8(xr, c, C);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += (float)v.e[e];
+        }
+        const float mean = row_sum<16>(sum, red[0], wave) * inv;
+        float sq = 0.0f;
+        for (int64_t c = 8 * (int64_t)threadIdx.x; c < C; c += 8192) {
+            const Vec8<T> v = load8(xr, c, C);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = (float)v.e[e] - mean;
+                sq += c + e < C ? d * d : 0.0f;
+            }
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<16>(sq, red[1], wave) * inv + eps);
+        if (threadIdx.x == 0) {
+            if (mean_out != nullptr) mean_out[r] = mean;
+            if (rstd_out != nullptr) rstd_out[r] = rstd;
+        }
+        for (int64_t c = 8 * (int64_t)threadIdx.x; c < C; c += 8192) {
+            const Vec8<T> v = load8(xr, c, C);
+            Vec8<P> wv, bv;
+            if (w != nullptr) wv = load8(w, c, C);
+            if (b != nullptr) bv = load8(b, c, C);
+            Vec8<T> o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float h = ((float)v.e[e] - mean) * rstd;
+                if (w != nullptr) h *= (float)wv.e[e];
+                if (b != nullptr) h += (float)bv.e[e];
+                o.e[e] = (T)h;
+            }
+            store8(y + r * C, c, C, o);
+        }
+    }
+}
+
+// One workgroup takes rows b, b + grid, ... in groups of kRows, writes dx and
+// keeps the column sums of dy h and dy; part: [grid][2][C].
+template <typename T, typename P, int NW, int U>
+__global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const T* __restrict__ x, const T* __restrict__ dy,
+                                                               const P* __restrict__ w, const float* __restrict__ mean,
+                                                               const float* __restrict__ rstd,
+                                                               const T* __restrict__ res, T* __restrict__ dx,
+                                                               float* __restrict__ part, int64_t rows, int C) {
+    constexpr int kRows = kBwdThreads / 64 / NW;
+    __shared__ float red[2][2][kBwdThreads / 64];
+    __shared__ float col[kRows > 1 ? NW * 512 : 1];
+    const int wave = threadIdx.x >> 6, c0 = ((wave % NW) * 64 + (threadIdx.x & 63)) * 8;
+    const float inv = 1.0f / (float)C;
+    float dw[U][8], db[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[u][e] = db[u][e] = 0.0f;
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < rows; r0 += (int64_t)gridDim.x * kRows, turn ^= 1) {
+        const int64_t r = r0 + wave / NW;
+        const bool live = r < rows;
+        const float mu = live ? mean[r] : 0.0f, rs = live ? rstd[r] : 0.0f;
+        Vec8<T> xv[U], gv[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            xv[u] = load8(x + r * C, c0 + u * NW * 512, live ? C : 0);
+            gv[u] = load8(dy + r * C, c0 + u * NW * 512, live ? C : 0);
+        }
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * NW * 512;
+            Vec8<P> wv;
+            if (w != nullptr) wv = load8(w, c, C);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                // past the row's end dy is 0 and x - mean is finite or the row's own
+                const float d = (float)gv[u].e[e], h = c + e < C && live ? ((float)xv[u].e[e] - mu) * rs : 0.0f;
+                const float g = w != nullptr ? d * (float)wv.e[e] : d;
+                s1 += g;
+                s2 += g * h;
+                dw[u][e] += d * h;
+                db[u][e] += d;
+            }
+        }
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        if (NW > 1) {
+            if ((threadIdx.x & 63) == 0) red[turn][0][wave] = s1, red[turn][1][wave] = s2;
+            __syncthreads();
+            const int first = wave / NW * NW;
+            s1 = s2 = 0.0f;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) s1 += red[turn][0][first + k], s2 += red[turn][1][first + k];
+        }
+        s1 *= inv;
+        s2 *= inv;
+        if (!live || dx == nullptr) continue;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * NW * 512;
+            if (c >= C) break;
+            Vec8<P> wv;
+            if (w != nullptr) wv = load8(w, c, C);
+            Vec8<T> rv, o;
+            if (res != nullptr) rv = load8(res + r * C, c, C);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = (float)gv[u].e[e], h = ((float)xv[u].e[e] - mu) * rs;
+                const float g = w != nullptr ? d * (float)wv.e[e] : d;
+                float v = (g - s1 - h * s2) * rs;
+                if (res != nullptr) v += (float)rv.e[e];
+                o.e[e] = (T)v;
+            }
+            store8(dx + r * C, c, C, o);
+        }
+    }
+    if (part == nullptr) return;
+    // the row groups' sums, in order, then one row of partials
+    float* out = part + (int64_t)blockIdx.x * 2 * C;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * NW * 512;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float(&acc)[8] = k == 0 ? dw[u] : db[u];
+            for (int g = 1; g < kRows; ++g) {
+                __syncthreads();
+                if (wave / NW == g)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) col[c0 + e] = acc[e];
+                __syncthreads();
+                if (wave / NW == 0)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[e] += col[c0 + e];
+            }
+            if (wave / NW == 0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < C) out[k * (int64_t)C + c + e] = acc[e];
+        }
+    }
+}
+
+// Rows too long for the registers: dx with one workgroup a row ...
+template <typename T, typename P>
+__global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const T* __restrict__ x, const T* __restrict__ dy,
+                                                             const P* __restrict__ w, const float* __restrict__ mean,
+                                                             const float* __restrict__ rstd, const T* __restrict__ res,
+                                                             T* __restrict__ dx, int64_t rows, int64_t C) {
+    __shared__ float red[2][16];
+    const int wave = threadIdx.x >> 6;
+    const float inv = 1.0f / (float)C;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const float mu = mean[r], rs = rstd[r];
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int64_t c = 8 * (int64_t)threadIdx.x; c < C; c += 8192) {
+            const Vec8<T> xv = load8(x + r * C, c, C), gv = load8(dy + r * C, c, C);
+            Vec8<P> wv;
+            if (w != nullptr) wv = load8(w, c, C);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float g = (float)gv.e[e] * (w != nullptr ? (float)wv.e[e] : 1.0f);
+                s1 += g;
+                s2 += c + e < C ? g * (((float)xv.e[e] - mu) * rs) : 0.0f;
+            }
+        }
+        s1 = row_sum<16>(s1, red[0], wave) * inv;
+        s2 = row_sum<16>(s2, red[1], wave) * inv;
+        for (int64_t c = 8 * (int64_t)threadIdx.x; c < C; c += 8192) {
+            const Vec8<T> xv = load8(x + r * C, c, C), gv = load8(dy + r * C, c, C);
+            Vec8<P> wv;
+            Vec8<T> rv, o;
+            if (w != nullptr) wv = load8(w, c, C);
+            if (res != nullptr) rv = load8(res + r * C, c, C);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float g = (float)gv.e[e] * (w != nullptr ? (float)wv.e[e] : 1.0f);
+                float v = (g - s1 - ((float)xv.e[e] - mu) * rs * s2) * rs;
+                if (res != nullptr) v += (float)rv.e[e];
+                o.e[e] = (T)v;
+            }
+            store8(dx + r * C, c, C, o);
+        }
+    }
+}
+
+// ... and the column sums, one workgroup for 512 columns and each of gridDim.y
+// shares of the rows; part: [gridDim.y][2][C].
+template <typename T>
+__global__ __launch_bounds__(64) void norm_cols_kernel(const T* __restrict__ x, const T* __restrict__ dy,
+                                                       const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                       float* __restrict__ part, int64_t rows, int64_t C) {
+    const int64_t c = ((int64_t)blockIdx.x * 64 + threadIdx.x) * 8;
+    if (c >= C) return;
+    float dw[8] = {}, db[8] = {};
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+        const float mu = mean[r], rs = rstd[r];
+        const Vec8<T> xv = load8(x + r * C, c, C), gv = load8(dy + r * C, c, C);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = (float)gv.e[e];
+            dw[e] += d * (((float)xv.e[e] - mu) * rs);
+            db[e] += d;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (c + e < C) {
+            part[(int64_t)blockIdx.y * 2 * C + c + e] = dw[e];
+            part[((int64_t)blockIdx.y * 2 + 1) * C + c + e] = db[e];
+        }
+}
+
+// dw and db from the rows of partials: 16 waves take every 16th row of 64
+// columns, then add up in order.
+template <typename P>
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict__ part, int n, int64_t C,
+                                                        P* __restrict__ dw, P* __restrict__ db) {
+    __shared__ float s[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    P* const out = blockIdx.y == 0 ? dw : db;
+    if (out == nullptr) return;
+    float v = 0.0f;
+    if (c < C)
+        for (int i = wave; i < n; i += 16) v += part[((int64_t)i * 2 + blockIdx.y) * C + c];
+    s[wave][lane] = v;
+    __syncthreads();
+    if (wave != 0 || c >= C) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) v += s[k][lane];
+    out[c] = (P)v;
+}
+
+constexpr int64_t kRegCols = 24576;              // the longest row held in registers
+constexpr int kMaxParts = 256;
+
+// Element type of the parameters: x's own or fp32.
+template <typename F>
+hipError_t with_types(DType x, DType p, F&& f) {
+    return with_type(x, [&](auto* t) {
+        if (p == DType::F32) return f(t, (float*)nullptr);
+        return f(t, t);
+    });
+}
+
+template <typename T, typename P, int NW, int U>
+hipError_t fwd(const T* x, int64_t rows, int64_t C, const P* w, const P* b, float eps, T* y, float* mean, float* rstd,
+               hipStream_t s) {
+    constexpr int kThreads = NW > 4 ? 64 * NW : 256, kRows = kThreads / 64 / NW;
+    const int64_t blocks = (rows + kRows - 1) / kRows;
+    hipLaunchKernelGGL((norm_fwd_kernel<T, P, NW, U>), dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))),
+                       dim3(kThreads), 0, s, x, w, b, y, mean, rstd, rows, (int)C, eps);
+    return hipGetLastError();
+}
+
+template <typename T, typename P, int NW, int U>
+hipError_t bwd(const T* x, const T* dy, int64_t rows, int64_t C, const P* w, const float* mean, const float* rstd,
+               const T* res, T* dx, float* part, int blocks, hipStream_t s) {
+    hipLaunchKernelGGL((norm_bwd_kernel<T, P, NW, U>), dim3((unsigned)blocks), dim3(kBwdThreads), 0, s, x, dy, w, mean,
+                       rstd, res, dx, part, rows, (int)C);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm(DType type, const void* x_, int64_t rows, int64_t C, DType ptype, const void* w_,
+                       const void* b_, float eps, void* y_, float* mean, float* rstd, hipStream_t s) {
+    return with_types(type, ptype, [&](auto* t, auto* p) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        using P = std::remove_pointer_t<decltype(p)>;
+        const T* x = (const T*)x_;
+        const P *w = (const P*)w_, *b = (const P*)b_;
+        T* y = (T*)y_;
+        if (C <= 512) return fwd<T, P, 1, 1>(x, rows, C, w, b, eps, y, mean, rstd, s);
+        if (C <= 1024) return fwd<T, P, 1, 2>(x, rows, C, w, b, eps, y, mean, rstd, s);
+        if (C <= 2048) return fwd<T, P, 4, 1>(x, rows, C, w, b, eps, y, mean, rstd, s);
+        if (C <= 4096) return fwd<T, P, 4, 2>(x, rows, C, w, b, eps, y, mean, rstd, s);
+        if (C <= 8192) return fwd<T, P, 4, 4>(x, rows, C, w, b, eps, y, mean, rstd, s);
+        if (C <= 16384) return fwd<T, P, 16, 2>(x, rows, C, w, b, eps, y, mean, rstd, s);
+        if (C <= kRegCols) return fwd<T, P, 16, 3>(x, rows, C, w, b, eps, y, mean, rstd, s);
+        hipLaunchKernelGGL((norm_fwd_long_kernel<T, P>), dim3((unsigned)(rows < (1 << 20) ? rows : (1 << 20))),
+                           dim3(1024), 0, s, x, w, b, y, mean, rstd, rows, C, eps);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_norm_grad(DType type, const void* x_, const void* dy_, int64_t rows, int64_t C, DType ptype,
+                            const void* w_, const float* mean, const float* rstd, const void* res_, void* dx_,
+                            void* dw, void* db, hipStream_t s) {
+    return with_types(type, ptype, [&](auto* t, auto* p) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        using P = std::remove_pointer_t<decltype(p)>;
+        const T *x = (const T*)x_, *dy = (const T*)dy_, *res = (const T*)res_;
+        const P* w = (const P*)w_;
+        T* dx = (T*)dx_;
+        const bool sums = dw != nullptr || db != nullptr;
+        // waves a row, and how many workgroups of 1024 threads take the rows
+        const int nw = C <= 512 ? 1 : C <= 1024 ? 2 : C <= 2048 ? 4 : C <= 4096 ? 4 : C <= 8192 ? 8 : 16;
+        const int64_t groups = (rows + 16 / nw - 1) / (16 / nw);
+        int parts = (int)(groups < kMaxParts ? groups : kMaxParts);
+        if (C > kRegCols) parts = (int)(rows < 64 ? rows : 64);
+        if (parts < 1) parts = 1;                    // no rows: sums of nothing
+        Workspace held;
+        float* part = nullptr;
+        hipError_t e = hipSuccess;
+        if (sums) e = held.take(kWsNorm, s, (size_t)parts * 2 * (size_t)C * sizeof(float), (void**)&part);
+        if (e != hipSuccess) return e;
+        if (C <= 512) e = bwd<T, P, 1, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= 1024) e = bwd<T, P, 2, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= 2048) e = bwd<T, P, 4, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= 4096) e = bwd<T, P, 4, 2>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= 8192) e = bwd<T, P, 8, 2>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= 16384) e = bwd<T, P, 16, 2>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= kRegCols) e = bwd<T, P, 16, 3>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else {
+            if (dx != nullptr && rows > 0)
+                hipLaunchKernelGGL((norm_bwd_long_kernel<T, P>), dim3((unsigned)(rows < (1 << 20) ? rows : (1 << 20))),
+                                   dim3(1024), 0, s, x, dy, w, mean, rstd, res, dx, rows, C);
+            e = hipGetLastError();
+            if (e == hipSuccess && sums) {
+                hipLaunchKernelGGL((norm_cols_kernel<T>), dim3((unsigned)((C + 511) / 512), (unsigned)parts), dim3(64),
+                                   0, s, x, dy, mean, rstd, part, rows, C);
+                e = hipGetLastError();
+            }
+        }
+        if (e != hipSuccess || !sums) return e;
+        hipLaunchKernelGGL((norm_sum_kernel<P>), dim3((unsigned)((C + 63) / 64), 2), dim3(1024), 0, s, part, parts, C,
+                           (P*)dw, (P*)db);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace ue5m3

@@ -1,0 +1,55 @@
+"""Dropout from a counter-based generator, as an autograd function and a
+module.  The mask is a function of (seed, tensor_id, element index): the
+backward pass computes it again, so nothing but the key is kept."""
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from .operators import dropout_forward
+
+
+class _DropoutFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, seed, tensor_id):
+        ctx.key = p, seed, tensor_id
+        return dropout_forward(x, p, seed, tensor_id, residual)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        dy = dy.contiguous()
+        dx = dropout_forward(dy, *ctx.key) if ctx.needs_input_grad[0] else None
+        return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
+
+
+def dropout(x, p, seed, tensor_id=0, residual=None):
+    """[``residual`` +] dropout of ``x`` (bf16, fp16 or fp32), with gradients.
+    ``p`` is taken to the nearest 2^-16; survivors are scaled by the
+    reciprocal of what is kept."""
+    x = x.contiguous()
+    residual = None if residual is None else residual.contiguous()
+    if torch.is_grad_enabled() and (x.requires_grad or (residual is not None and residual.requires_grad)):
+        return _DropoutFn.apply(x, residual, float(p), int(seed), int(tensor_id))
+    return dropout_forward(x, p, seed, tensor_id, residual)
+
+
+class Dropout(torch.nn.Module):
+    """Dropout with its own key: call c of the module in training draws with
+    key ``seed`` + c and tensor id ``layer_id``; in evaluation x (plus the
+    residual) passes."""
+
+    def __init__(self, p=0.1, seed=0, layer_id=0):
+        super().__init__()
+        if not 0.0 <= p <= 1.0:
+            raise ValueError("p must be in [0, 1]")
+        self.p, self.seed, self.layer_id, self.calls = float(p), int(seed), int(layer_id), 0
+
+    def forward(self, x, residual=None):
+        if not self.training:
+            return x if residual is None else residual + x
+        key = (self.seed + self.calls) & (2 ** 64 - 1)
+        self.calls += 1
+        return dropout(x, self.p, key, self.layer_id, residual)
+
+    def extra_repr(self):
+        return f"p={self.p}"
