@@ -1,6 +1,7 @@
 // C ABI shim of the operators around the linear layers (layer norm, dropout,
 // the products in 8-bit floating point): argument validation, status mapping
 // and dispatch.  See include/ue5m3.h for the contract of every entry point.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -24,6 +25,8 @@ inline bool known(ue5m3_out_t t) { return t == UE5M3_OUT_F32 || t == UE5M3_OUT_B
 inline uintptr_t size_of(ue5m3_dtype_t t) { return t == UE5M3_F32 ? 4 : 2; }
 inline DType dtype(ue5m3_dtype_t t) { return static_cast<DType>(t); }
 inline int64_t blocks(int64_t n) { return (n + 127) / 128; }
+// Whether the quantizers' grids take a [rows, cols] tensor (16 rows a workgroup).
+inline bool fits(int64_t rows, int64_t cols) { return (rows + 15) / 16 <= kMaxGrid / std::max<int64_t>(blocks(cols), 1); }
 
 // Types, sizes and parameters common to layer norm and its gradient.
 ue5m3_status_t norm_args(int64_t rows, int64_t cols, ue5m3_dtype_t xt, ue5m3_dtype_t pt) {
@@ -95,7 +98,7 @@ ue5m3_status_t ue5m3_quantize_fp8(const void* x, int64_t rows, int64_t cols, ue5
         return UE5M3_EINVAL;
     if (rows < 0 || cols < 0) return UE5M3_ESHAPE;
     if (rows == 0 || cols == 0) return UE5M3_OK;
-    if (blocks(rows) > kMaxGrid / blocks(cols)) return UE5M3_ESHAPE;
+    if (!fits(rows, cols)) return UE5M3_ESHAPE;
     if (x == nullptr || (payload_r == nullptr && payload_c == nullptr)) return UE5M3_EINVAL;
     if (!aligned(x, size_of(x_type)) || !aligned(payload_r, 16) || !aligned(scales_r, 16) || !aligned(payload_c, 16) ||
         !aligned(scales_c, 16))
@@ -110,7 +113,7 @@ ue5m3_status_t ue5m3_quantize_fp8_tiles(const void* w, int64_t rows, int64_t col
     if (!known(w_type) || !known(scale_kind) || (payload_t == nullptr) != (scales_t == nullptr)) return UE5M3_EINVAL;
     if (rows < 0 || cols < 0) return UE5M3_ESHAPE;
     if (rows == 0 || cols == 0) return UE5M3_OK;
-    if (blocks(rows) > kMaxGrid / blocks(cols)) return UE5M3_ESHAPE;
+    if (!fits(rows, cols)) return UE5M3_ESHAPE;
     if (w == nullptr || payload == nullptr || scales == nullptr) return UE5M3_EINVAL;
     if (!aligned(w, size_of(w_type)) || !aligned(payload, 16) || !aligned(scales, 16) || !aligned(payload_t, 16) ||
         !aligned(scales_t, 16))
@@ -147,7 +150,7 @@ ue5m3_status_t ue5m3_linear_fp8(const void* x_bf16, int64_t T, int64_t K, int64_
     if (!known(scale_kind) || !known(y_type)) return UE5M3_EINVAL;
     if (T < 0 || N < 0 || K < 0 || K > kMaxK) return UE5M3_ESHAPE;
     if (T == 0 || N == 0) return UE5M3_OK;
-    if (blocks(T) > kMaxGrid / blocks(N) || blocks(T) > kMaxGrid / blocks(K + 1)) return UE5M3_ESHAPE;
+    if (blocks(T) > kMaxGrid / blocks(N) || !fits(T, K)) return UE5M3_ESHAPE;
     if (y == nullptr || (K > 0 && (x_bf16 == nullptr || w == nullptr || w_scales == nullptr))) return UE5M3_EINVAL;
     if (!aligned(y, 16) || (K > 0 && (!aligned(x_bf16, 2) || !aligned(w, 16) || !aligned(w_scales, 16))))
         return UE5M3_EALIGN;

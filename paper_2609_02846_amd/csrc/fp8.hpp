@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace ue5m3 {
 namespace {
 
@@ -13,6 +15,20 @@ constexpr float kE4M3Top = 448.0f, kE5M2Top = 57344.0f;
 // Elements of one row of a 1D scale array (one row for each block of 128):
 // whole groups of 16, so that a kernel's vector loads stay aligned.
 __host__ __device__ __forceinline__ int64_t scale_pitch(int64_t rows) { return (rows + 15) / 16 * 16; }
+
+// Largest of the 16 lanes of a DPP row, in each of them.
+__device__ __forceinline__ float row16_max(float v) {
+    auto step = [&](auto ctl) {
+        constexpr int kCtl = decltype(ctl)::value;
+        const int o = __builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtl, 0xF, 0xF, false);
+        v = fmaxf(v, __int_as_float(o));
+    };
+    step(std::integral_constant<int, 0x128>{});      // rotate right by 8, 4, 2, 1
+    step(std::integral_constant<int, 0x124>{});
+    step(std::integral_constant<int, 0x122>{});
+    step(std::integral_constant<int, 0x121>{});
+    return v;
+}
 
 // |x|, or 0 for an infinity or a NaN.
 __device__ __forceinline__ float finite_abs(float x) {

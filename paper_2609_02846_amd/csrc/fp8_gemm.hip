@@ -9,103 +9,140 @@
 // sa sb times it is added to the accumulators, in binary32.  The products are
 // issued as B x A^T: a lane then holds four consecutive columns n of one row m,
 // so sa is one value a lane.
+#include <algorithm>
+
 #include "fp8.hpp"
+#include "fp8_tile.hpp"
 #include "gemm_regs.hpp"
 #include "launch.hpp"
 
 namespace ue5m3 {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 constexpr int kTile = 128, kRowBytes = 128, kStage = 2 * kTile * kRowBytes;
 
-// A lane's 32 bytes of row `row`: chunks g and g + 4 of eight, which lie at
-// their number XOR row % 8.  Which k they are does not matter as long as both
-// operands agree.
-__device__ __forceinline__ i32x8 read_frag(const uint8_t* rows, int row, int g) {
-    const uint8_t* p = rows + row * kRowBytes;
-    const uint4 lo = *reinterpret_cast<const uint4*>(p + ((g ^ (row & 7)) * 16));
-    const uint4 hi = *reinterpret_cast<const uint4*>(p + (((g + 4) ^ (row & 7)) * 16));
-    return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+// 128 x 128 output tiles, four waves of 64 x 64, a ring of kRing stages of one
+// block each.  While a wave multiplies a stage out of registers it reads the
+// next one from LDS, and the stages after that are on their way: at the barrier
+// that opens turn k, stage k + 1 has landed and stage k has left the LDS, so
+// stage k + kRing takes its place.  Scales travel with their stage, one dword
+// for each row (an E8M0 byte is loaded as one).
+constexpr int kRing = 4, kScaleBytes = 4 * 256, kStageAll = kStage + kScaleBytes;
+constexpr int kLoads = 9;                            // of a wave for one stage: 8 of rows, 1 of scales
+
+// One dword (E8: byte) a lane from rsrc at voff + soff to LDS at lds + 4 lane.
+template <bool E8>
+__device__ __forceinline__ void dma_scale(i32x4_t rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
+    if (E8)
+        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_ubyte %0, %1, %2 offen lds"
+                     :: "v"(voff), "s"(rsrc), "s"(soff), "s"(lds) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dword %0, %1, %2 offen lds"
+                     :: "v"(voff), "s"(rsrc), "s"(soff), "s"(lds) : "memory", "m0");
 }
 
-template <bool OUT_BF16>
-__device__ __forceinline__ void store4(void* C, int64_t m, int64_t n, int64_t N, const f32x4& v) {
-    if (OUT_BF16) {
-        uint16_t* d = (uint16_t*)C + m * N + n;
-        const uint32_t lo = pack_bf16x2(v[0], v[1]), hi = pack_bf16x2(v[2], v[3]);
-        if (n + 4 <= N) {
-            const uint2 w = make_uint2(lo, hi);
-            __builtin_memcpy(d, &w, 8);
-        } else {
-            if (n < N) d[0] = (uint16_t)lo;
-            if (n + 1 < N) d[1] = (uint16_t)(lo >> 16);
-            if (n + 2 < N) d[2] = (uint16_t)hi;
-        }
-    } else {
-        float* d = (float*)C + m * N + n;
-        if (n + 4 <= N) {
-            __builtin_memcpy(d, &v, 16);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (n + e < N) d[e] = v[e];
-        }
-    }
+// One product from zero, into registers that a VALU instruction can read (the
+// compiler's own choice are accumulation registers, from where each value is
+// moved first).  It does not model this instruction: a product of 8 passes may be
+// read 12 instructions later, which the callers' order keeps.
+template <int AF>
+__device__ __forceinline__ void product(f32x4& d, const i32x8& b, const i32x8& a) {
+    if (AF == 0)
+        asm volatile("v_mfma_f32_16x16x128_f8f6f4 %0, %1, %2, 0" : "=&v"(d) : "v"(b), "v"(a));
+    else
+        asm volatile("v_mfma_f32_16x16x128_f8f6f4 %0, %1, %2, 0 blgp:1" : "=&v"(d) : "v"(b), "v"(a));
 }
 
-// 128 x 128 output tiles, four waves of 64 x 64, two stages of one block each.
+// One product times 2^(eb - 127) 2^(ea - 127), added in place (see product()).
+template <int AF>
+__device__ __forceinline__ void accumulate(f32x4& d, const i32x8& b, const i32x8& a, int eb, int ea) {
+    if (AF == 0)
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+                     : "+v"(d) : "v"(b), "v"(a), "v"(eb), "v"(ea));
+    else
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] blgp:1"
+                     : "+v"(d) : "v"(b), "v"(a), "v"(eb), "v"(ea));
+}
+
+// Registers of one stage: a lane's share of 64 rows of each operand, and their
+// scales (E8: codes; else sa of each A row and, for 1D, sb of four rows).
+template <bool E8, bool TILED>
+struct Frag {
+    i32x8 a[4], b[4];
+    float sa[4];
+    f32x4 sb[TILED || E8 ? 1 : 4];
+    int ea[4], eb[4];
+};
+
 template <int AF, bool E8, bool TILED, bool OUT_BF16>
-__global__ __launch_bounds__(256, 2) void gemm_fp8_kernel(int64_t M, int64_t N, int64_t KB, int64_t tiles_n,
+__global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, int KB, int tiles_n,
                                                           const uint8_t* __restrict__ A, const void* __restrict__ As,
                                                           const uint8_t* __restrict__ B, const void* __restrict__ Bs,
-                                                          void* __restrict__ C) {
-    __shared__ __attribute__((aligned(16))) uint8_t sP[2 * kStage];
+                                                          void* __restrict__ C, int parts, float* __restrict__ part) {
+    __shared__ __attribute__((aligned(16))) uint8_t sP[kRing * kStageAll];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1, l16 = lane & 15, g = lane >> 4;
-    const int64_t m0 = (int64_t)blockIdx.x / tiles_n * kTile, n0 = (int64_t)blockIdx.x % tiles_n * kTile;
+    // (divisions run in vector registers: back to scalars)
+    const int item = uniform((int)blockIdx.x / parts), p = (int)blockIdx.x - item * parts;
+    const int tm = uniform(item / tiles_n), tn = item - tm * tiles_n;
+    const int64_t m0 = (int64_t)tm * kTile, n0 = (int64_t)tn * kTile;
+    const int kb0 = uniform(KB * p / parts), kb1 = uniform(KB * (p + 1) / parts);
     const uint32_t Kp = (uint32_t)KB * 128u;
+    constexpr uint32_t kEl = E8 ? 1 : 4;
 
     // waves 0, 1 bring A rows, waves 2, 3 B rows: 64 rows each, 8 rows a load
     const bool isA = wave < 2;
-    const int64_t left = isA ? M - m0 : N - n0;
-    const i32x4_t src = buffer_rsrc(isA ? A + m0 * Kp : B + n0 * Kp, (uint32_t)(left < kTile ? left : kTile) * Kp);
+    const int64_t x0 = isA ? m0 : n0, rows = isA ? M : N, left = rows - x0;
+    const i32x4_t src =
+        buffer_rsrc((isA ? A : B) + x0 * Kp, (uint32_t)uniform((int)(left < kTile ? left : kTile)) * Kp);
     const uint32_t voff = (uint32_t)(64 * (wave & 1) + (lane >> 3)) * Kp + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
-    const uint32_t lds = lds_addr(sP) + (uint32_t)wave * 64u * kRowBytes;
-    auto load = [&](int64_t kb, int buf) {
-        const uint32_t vo = voff + (uint32_t)kb * 128u, to = lds + (uint32_t)(buf * kStage);
-        static_for<0, 8>([&](auto ic) {
-            constexpr int i = decltype(ic)::value;
-            dma_buf_x4<i * 1024>(src, vo + i * 8 * Kp, 0u, to);
-        });
+    const uint32_t lds = lds_addr(sP) + (uint32_t)wave * 64u * kRowBytes, lds_s = lds_addr(sP) + kStage + wave * 256u;
+    // scales of 64 rows of the wave's operand, one row of the array a stage; of
+    // a tile, the one scale
+    const bool tile_scale = TILED && !isA;
+    const int64_t sstep = (tile_scale ? 1 : scale_pitch(rows)) * kEl;
+    const uint8_t* const sbase = (const uint8_t*)(isA ? As : Bs) + (tile_scale ? (int64_t)tn * KB : x0) * kEl;
+    const uint32_t srow = tile_scale ? 0u : (uint32_t)min((int64_t)(64 * (wave & 1) + lane), left - 1) * kEl;
+    // load i of stage kb: rows 8i .. 8i + 7, then the scales
+    auto load = [&](auto ic, int kb, int slot) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (i < 8) {
+            dma_buf_x4<i * 1024>(src, voff + (uint32_t)kb * 128u + i * 8 * Kp, 0u, lds + (uint32_t)(slot * kStageAll));
+        } else {
+            dma_scale<E8>(buffer_rsrc(sbase + kb * sstep, kTile * kEl), srow, 0u, lds_s + (uint32_t)(slot * kStageAll));
+        }
     };
-
-    const int64_t pa = scale_pitch(M), pb = scale_pitch(N), nb = n0 / 128;
-    float fa[4], fb[E8 || TILED ? 1 : 16];
-    int ea[4], eb[4];
-    auto scales = [&](int64_t kb) {
+    using F = Frag<E8, TILED>;
+    const uint8_t* const pa = sP + (wm * 64 + l16) * kRowBytes;
+    const uint8_t* const pb = sP + (kTile + wn * 64 + l16) * kRowBytes;
+    const int c0 = (g ^ (l16 & 7)) * 16, c1 = ((g + 4) ^ (l16 & 7)) * 16;
+    // half h of a lane's 32 bytes of row group i: chunks g and g + 4 of eight,
+    // which lie at their number XOR row % 8 (which k they are does not matter
+    // as long as both operands agree)
+    auto frag = [&](i32x8& f, const uint8_t* base, int i, int h, int slot) {
+        const uint4 v = *reinterpret_cast<const uint4*>(base + slot * kStageAll + i * 16 * kRowBytes + (h ? c1 : c0));
+        f[4 * h] = (int)v.x; f[4 * h + 1] = (int)v.y; f[4 * h + 2] = (int)v.z; f[4 * h + 3] = (int)v.w;
+    };
+    auto read_scales = [&](F& f, int slot) {
+        const uint8_t* const s = sP + slot * kStageAll + kStage;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t m = min(m0 + wm * 64 + 16 * i + l16, M - 1);
-            if (E8) ea[i] = ((const uint8_t*)As)[kb * pa + m];
-            else fa[i] = ((const float*)As)[kb * pa + m];
-        }
-        if (TILED) {
-            if (E8) eb[0] = ((const uint8_t*)Bs)[nb * KB + kb];
-            else fb[0] = ((const float*)Bs)[nb * KB + kb];
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
+            const uint8_t* at = s + wm * 256 + (16 * i + l16) * 4;
+            if (E8) f.ea[i] = *reinterpret_cast<const int*>(at);
+            else f.sa[i] = *reinterpret_cast<const float*>(at);
             if (E8) {
-                eb[j] = ((const uint8_t*)Bs)[kb * pb + min(n0 + wn * 64 + 16 * j + l16, N - 1)];
-            } else {
-                const float4 v = *reinterpret_cast<const float4*>((const float*)Bs + kb * pb +
-                                                                  min(n0 + wn * 64 + 16 * j + 4 * g, pb - 4));
-                fb[4 * j] = v.x; fb[4 * j + 1] = v.y; fb[4 * j + 2] = v.z; fb[4 * j + 3] = v.w;
+                if (!TILED || i == 0) f.eb[i] = *reinterpret_cast<const int*>(s + (2 + wn) * 256 + (TILED ? 0 : 16 * i + l16) * 4);
+            } else if (!TILED) {
+                f.sb[i] = *reinterpret_cast<const f32x4*>(s + (2 + wn) * 256 + (16 * i + 4 * g) * 4);
             }
+        }
+        if (TILED && !E8) {
+            const float t = *reinterpret_cast<const float*>(s + 2 * 256);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.sa[i] *= t;
         }
     };
 
@@ -115,33 +152,78 @@ __global__ __launch_bounds__(256, 2) void gemm_fp8_kernel(int64_t M, int64_t N, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    if (KB > 0) load(0, 0);
-    for (int64_t kb = 0; kb < KB; ++kb) {
-        // this stage has landed everywhere and every wave has left the other
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        scales(kb);
-        if (kb + 1 < KB) load(kb + 1, (int)(kb + 1) & 1);
-        const uint8_t* const rows = sP + ((int)kb & 1) * kStage;
-        i32x8 a[4];
+    // 16 products of stage registers f; between them the next stage is read into
+    // n and the loads of stage `kb` are issued.  A binary32 product is added three
+    // products later, when it has left the matrix pipe (at least 14 instructions
+    // after its own, whatever else stands between them).
+    auto turn = [&](F& f, F& n, int slot, int kb, int to) {
+        f32x4 q[E8 ? 1 : 4];
+        auto add = [&](auto xc) {
+            constexpr int x = decltype(xc)::value, j = x / 4, i = x % 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = read_frag(rows, wm * 64 + 16 * i + l16, g);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const i32x8 b = read_frag(rows, kTile + wn * 64 + 16 * j + l16, g);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (E8) {
-                    acc[j][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a[i], acc[j][i], 0, AF, 0,
-                                                                                eb[TILED ? 0 : j], 0, ea[i]);
-                } else {
-                    const f32x4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        b, a[i], f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, AF, 0, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        acc[j][i][e] = __builtin_fmaf(p[e], fa[i] * fb[TILED ? 0 : 4 * j + e], acc[j][i][e]);
-                }
-            }
+            for (int e = 0; e < 4; ++e)
+                acc[j][i][e] = __builtin_fmaf(q[E8 ? 0 : x % 4][e], TILED ? f.sa[i] : f.sa[i] * f.sb[TILED || E8 ? 0 : j][e], acc[j][i][e]);
+        };
+        read_scales(n, slot);
+        static_for<0, 16>([&](auto xc) {
+            constexpr int x = decltype(xc)::value, j = x / 4, i = x % 4;
+            if constexpr (E8)
+                accumulate<AF>(acc[j][i], f.b[j], f.a[i], f.eb[TILED ? 0 : j], f.ea[i]);
+            else
+                product<AF>(q[x % 4], f.b[j], f.a[i]);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (x < 9) load(xc, kb, to);
+            frag(x < 8 ? n.a[x / 2 % 4] : n.b[x / 2 % 4], x < 8 ? pa : pb, x / 2 % 4, x % 2, slot);
+            if constexpr (!E8 && x >= 3) add(std::integral_constant<int, x - 3>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (!E8) {
+            asm volatile("s_nop 11");                // the last three leave the matrix pipe
+            __builtin_amdgcn_sched_barrier(0);
+            add(std::integral_constant<int, 13>{});
+            add(std::integral_constant<int, 14>{});
+            add(std::integral_constant<int, 15>{});
         }
+    };
+
+    const int n = kb1 - kb0;
+    // past the last stage that one is loaded and read again, unused, so that the
+    // waits count the same loads in every turn
+    if (n > 0) {
+#pragma unroll
+        for (int k = 0; k < kRing; ++k)
+            static_for<0, kLoads>([&](auto ic) { load(ic, min(kb0 + k, kb1 - 1), k); });
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads * (kRing - 1)) : "memory");
+        F f, h;
+        read_scales(f, 0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            frag(f.a[i / 2], pa, i / 2, i % 2, 0);
+            frag(f.b[i / 2], pb, i / 2, i % 2, 0);
+        }
+        auto step = [&](F& cur, F& nxt, int k) {
+            // stage k + 1 has landed everywhere, every wave holds stage k
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads * (kRing - 2)) : "memory");
+            turn(cur, nxt, (k + 1) % kRing, min(kb0 + k + kRing, kb1 - 1), k % kRing);
+        };
+        int k = 0;
+        for (; k + 1 < n; k += 2) {
+            step(f, h, k);
+            step(h, f, k + 1);
+        }
+        if (k < n) step(f, h, k);
+        // no load outlives the kernel's LDS, and the last products have landed
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (parts > 1) {
+        // this part's sums as [item][part][wave][j][i][lane][4]
+        float* out = part + ((int64_t)item * parts + p) * (kTile * kTile) + wave * 4096 + lane * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(out + (j * 4 + i) * 256) = acc[j][i];
+        return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -152,15 +234,48 @@ __global__ __launch_bounds__(256, 2) void gemm_fp8_kernel(int64_t M, int64_t N, 
     }
 }
 
+// The parts' sums of one sixteenth of a tile, in order.
+template <bool OUT_BF16>
+__global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(int64_t M, int64_t N, int64_t tiles_n, void* __restrict__ C,
+                                                           int parts, const float* __restrict__ part) {
+    const int64_t item = blockIdx.x / 16;
+    const int at = (blockIdx.x % 16) * 256 + threadIdx.x, lane = at & 63, ji = at >> 6 & 15, wave = at >> 10;
+    const float* in = part + item * parts * (kTile * kTile) + at * 4;
+    f32x4 v = *reinterpret_cast<const f32x4*>(in);
+    for (int p = 1; p < parts; ++p) v += *reinterpret_cast<const f32x4*>(in + (int64_t)p * (kTile * kTile));
+    const int64_t m = item / tiles_n * kTile + (wave >> 1) * 64 + (ji & 3) * 16 + (lane & 15);
+    const int64_t n = item % tiles_n * kTile + (wave & 1) * 64 + (ji >> 2) * 16 + (lane >> 4) * 4;
+    if (m < M) store4<OUT_BF16>(C, m, n, N, v);
+}
+
 }  // namespace
 
 hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
                            const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16,
                            hipStream_t s) {
     const int64_t KB = (K + 127) / 128, tm = (M + kTile - 1) / kTile, tn = (N + kTile - 1) / kTile;
+    if (fp8_skinny(M, K)) return launch_gemm_fp8_skinny(M, N, K, a, as, a_fmt, b, bs, tiled, e8, c, c_bf16, s);
+    // split along K while that still gives every CU at most one part of at
+    // least eight stages
+    int cus = 0;
+    hipError_t err = device_cus(&cus);
+    if (err != hipSuccess) return err;
+    int64_t parts = std::min<int64_t>(cus / std::max<int64_t>(tm * tn, 1), KB / 8);
+    if (parts < 1) parts = 1;
+    Workspace held;                                  // until the sum is enqueued
+    float* part = nullptr;
+    if (parts > 1) {
+        err = held.take(kWsFp8, s, (size_t)(tm * tn * parts) * kTile * kTile * 4, (void**)&part);
+        if (err != hipSuccess) return err;
+    }
     auto go = [&](auto af, auto e, auto tl, auto bf) {
         hipLaunchKernelGGL((gemm_fp8_kernel<decltype(af)::value, decltype(e)::value, decltype(tl)::value, decltype(bf)::value>),
-                           dim3((unsigned)(tm * tn)), dim3(256), 0, s, M, N, KB, tn, a, as, b, bs, c);
+                           dim3((unsigned)(tm * tn * parts)), dim3(256), 0, s, M, N, (int)KB, (int)tn, a, as, b, bs, c,
+                           (int)parts, part);
+        hipError_t e2 = hipGetLastError();
+        if (e2 != hipSuccess || parts == 1) return e2;
+        hipLaunchKernelGGL((gemm_fp8_sum_kernel<decltype(bf)::value>), dim3((unsigned)(tm * tn * 16)), dim3(256), 0, s,
+                           M, N, tn, c, (int)parts, part);
         return hipGetLastError();
     };
     using Y = std::true_type;
@@ -175,6 +290,7 @@ hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, co
 
 hipError_t launch_linear_fp8(const void* x, int64_t T, int64_t K, int64_t N, const uint8_t* w, const void* ws,
                              bool e8, void* y, bool y_bf16, hipStream_t s) {
+    if (fp8_fused(T, K)) return launch_linear_fp8_fused(x, T, K, N, w, ws, e8, y, y_bf16, s);
     const int64_t KB = (K + 127) / 128;
     const size_t payload = (size_t)(T * KB * 128), scales = (size_t)(KB * scale_pitch(T)) * (e8 ? 1 : 4);
     Workspace held;                                  // until the product is enqueued

@@ -28,22 +28,8 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Largest of the 16 lanes of a DPP row, in each of them.
-__device__ __forceinline__ float row16_max(float v) {
-    auto step = [&](auto ctl) {
-        constexpr int kCtl = decltype(ctl)::value;
-        const int o = __builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtl, 0xF, 0xF, false);
-        v = fmaxf(v, __int_as_float(o));
-    };
-    step(std::integral_constant<int, 0x128>{});      // rotate right by 8, 4, 2, 1
-    step(std::integral_constant<int, 0x124>{});
-    step(std::integral_constant<int, 0x122>{});
-    step(std::integral_constant<int, 0x121>{});
-    return v;
-}
-
 // Which outputs a launch writes.
-enum class Form : int { Rows, Cols, Dual, Tiles, TilesT };
+enum class Form : int { Rows, Cols, Dual, Tiles, TilesT };   // Rows: a kernel of its own
 
 struct QuantOut {
     uint8_t *rows, *cols;                            // payloads [R][pad(C)], [C][pad(R)]
@@ -61,7 +47,7 @@ __device__ __forceinline__ void put_scale(void* p, int64_t i, const BlockScale<E
 template <typename T, bool E5M2, bool E8, Form F>
 __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict__ x, int64_t R, int64_t C,
                                                              int64_t blocks_c, QuantOut out) {
-    constexpr bool kRows = F == Form::Rows || F == Form::Dual, kCols = F == Form::Cols || F == Form::Dual;
+    constexpr bool kRows = F == Form::Dual, kCols = F == Form::Cols || F == Form::Dual;
     constexpr bool kTiles = F == Form::Tiles || F == Form::TilesT, kT = kCols || F == Form::TilesT;
     __shared__ float smax[4][128];
     __shared__ __attribute__((aligned(16))) uint8_t sT[kT ? 128 * 128 : 16];
@@ -155,6 +141,30 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict
     }
 }
 
+// Row blocks alone: 16 lanes a block, one block a thread group, so that a few
+// rows still spread over many waves.  A workgroup takes 16 rows of one block
+// column (the rows' scales are neighbours).
+template <typename T, bool E5M2, bool E8>
+__global__ __launch_bounds__(kThreads) void quant_fp8_rows_kernel(const T* __restrict__ x, int64_t R, int64_t C,
+                                                                  int64_t blocks_c, uint8_t* __restrict__ out,
+                                                                  void* __restrict__ scales) {
+    const int t = threadIdx.x & 15;
+    const int64_t br = (int64_t)blockIdx.x / blocks_c, bc = (int64_t)blockIdx.x % blocks_c;
+    const int64_t r = br * 16 + (threadIdx.x >> 4), c = bc * 128 + t * 8;
+    const Vec8<T> v = load8(x + r * C, c, r < R ? C : 0);
+    float a = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) a = fmaxf(a, finite_abs((float)v.e[j]));
+    const BlockScale<E8> s = BlockScale<E8>::of(row16_max(a), E5M2);
+    if (r >= R) return;
+    float q[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = s.value((float)v.e[j]);
+    *reinterpret_cast<uint2*>(out + r * (blocks_c * 128) + c) =
+        make_uint2(pack_fp8<E5M2>(q[0], q[1], q[2], q[3]), pack_fp8<E5M2>(q[4], q[5], q[6], q[7]));
+    if (t == 0) put_scale(scales, bc * scale_pitch(R) + r, s);
+}
+
 template <Form F>
 hipError_t launch(DType type, bool e5m2, bool e8, const void* x, int64_t R, int64_t C, const QuantOut& out,
                   hipStream_t s) {
@@ -162,8 +172,13 @@ hipError_t launch(DType type, bool e5m2, bool e8, const void* x, int64_t R, int6
     return with_type(type, [&](auto* tp) {
         using T = std::remove_pointer_t<decltype(tp)>;
         auto go = [&](auto f5, auto f8) {
-            hipLaunchKernelGGL((quant_fp8_kernel<T, decltype(f5)::value, decltype(f8)::value, F>),
-                               dim3((unsigned)(br * bc)), dim3(kThreads), 0, s, (const T*)x, R, C, bc, out);
+            if constexpr (F == Form::Rows)
+                hipLaunchKernelGGL((quant_fp8_rows_kernel<T, decltype(f5)::value, decltype(f8)::value>),
+                                   dim3((unsigned)((R + 15) / 16 * bc)), dim3(kThreads), 0, s, (const T*)x, R, C, bc,
+                                   out.rows, out.rows_scale);
+            else
+                hipLaunchKernelGGL((quant_fp8_kernel<T, decltype(f5)::value, decltype(f8)::value, F>),
+                                   dim3((unsigned)(br * bc)), dim3(kThreads), 0, s, (const T*)x, R, C, bc, out);
             return hipGetLastError();
         };
         using Y = std::true_type;

@@ -1624,15 +1624,6 @@ hipError_t launch_one(int64_t M, int64_t N, int64_t K, const uint8_t* a, const u
     return hipGetLastError();
 }
 
-// Compute units of the current device.
-hipError_t device_cus(int* cus) {
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e == hipSuccess) e = hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev);
-    if (e == hipSuccess && *cus <= 0) e = hipErrorInvalidDevice;
-    return e;
-}
-
 // Modelled time (us) of the 256 x 256-tile kernel, for the choice between it
 // and the smaller tiles: whole rounds of one tile per CU plus a last one
 // that is split where launch_reg splits it, each with a fixed part (pipeline
@@ -1706,6 +1697,14 @@ hipError_t launch_mode(int cus, int64_t M, int64_t N, int64_t K, const uint8_t* 
 }
 
 }  // namespace
+
+hipError_t device_cus(int* cus) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev);
+    if (e == hipSuccess && *cus <= 0) e = hipErrorInvalidDevice;
+    return e;
+}
 
 hipError_t launch_gemm(BScale bmode, float amul, int64_t M, int64_t N, int64_t K, const uint8_t* a,
                        const uint8_t* a_scales, const float* a_dec, const uint8_t* b,

@@ -27,8 +27,9 @@ enum class Fp8 : int { E4M3 = 0, E5M2 = 1 };
 // not freed, until the process ends): split-tile partials of the GEMMs,
 // block-32 scales expanded to the block-16 layout, per-workgroup partial
 // maxima of the amax kernels, per-workgroup column sums of layer norm's
-// backward pass, the quantized tokens of a serving call.
-enum WorkspaceKind : int { kWsSplit = 0, kWsScales = 1, kWsAmax = 2, kWsNorm = 3, kWsTokens = 4, kWsKinds = 5 };
+// backward pass, the quantized tokens of a serving call, split partials of the
+// 8-bit products.
+enum WorkspaceKind : int { kWsSplit = 0, kWsScales = 1, kWsAmax = 2, kWsNorm = 3, kWsTokens = 4, kWsFp8 = 5, kWsKinds = 6 };
 
 // One call's use of a workspace.  Uses on one stream are ordered by the
 // stream as long as each call's launches are enqueued together, so the
@@ -185,10 +186,23 @@ hipError_t launch_quant_fp8(DType type, Fp8 fmt, bool e8, const void* x, int64_t
 hipError_t launch_quant_fp8_tiles(DType type, bool e8, const void* w, int64_t R, int64_t C, uint8_t* payload,
                                   void* scales, uint8_t* payload_t, void* scales_t, hipStream_t s);
 
+// Compute units of the current device.
+hipError_t device_cus(int* cus);
+
 // C [M, N] from operands in blocks of 128 along K; tiled: one B scale for 128
 // rows; B is E4M3.
 hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
                            const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16, hipStream_t s);
+
+// The same for few rows (whether it takes them: fp8_skinny), and with bf16
+// tokens that the kernel quantizes itself (fp8_fused).
+bool fp8_skinny(int64_t M, int64_t K);
+hipError_t launch_gemm_fp8_skinny(int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
+                                  const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16,
+                                  hipStream_t s);
+bool fp8_fused(int64_t T, int64_t K);
+hipError_t launch_linear_fp8_fused(const void* x_bf16, int64_t T, int64_t K, int64_t N, const uint8_t* w,
+                                   const void* ws, bool e8, void* y, bool y_bf16, hipStream_t s);
 
 // y [T, N] = x [T, K] times a weight in tiles, transposed: quantizes x to a
 // workspace, then the product.
