@@ -21,6 +21,9 @@ namespace {
 
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
+    return (uint64_t)(uint32_t)uniform((int)(uint32_t)(v >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)v);
+}
 
 constexpr int kTile = 128, kRowBytes = 128, kStage = 2 * kTile * kRowBytes;
 
@@ -33,15 +36,24 @@ constexpr int kTile = 128, kRowBytes = 128, kStage = 2 * kTile * kRowBytes;
 constexpr int kRing = 4, kScaleBytes = 4 * 256, kStageAll = kStage + kScaleBytes;
 constexpr int kLoads = 9;                            // of a wave for one stage: 8 of rows, 1 of scales
 
-// One dword (E8: byte) a lane from rsrc at voff + soff to LDS at lds + 4 lane.
+// Direct loads to LDS that cost one instruction each: m0 holds the LDS address,
+// and the immediate offset counts for both sides (so a lane's source offset is
+// less by it).  The instructions between a write of m0 and a load that takes it
+// are the callers' matter: a wait state is needed there.
+__device__ __forceinline__ void set_m0(uint32_t lds) { asm volatile("s_mov_b32 m0, %0" :: "s"(lds) : "memory", "m0"); }
+
+template <int OFF>
+__device__ __forceinline__ void dma_rows(i32x4_t rsrc, uint32_t voff, uint32_t soff) {
+    asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" :: "v"(voff), "s"(rsrc), "s"(soff), "n"(OFF) : "memory");
+}
+
+// One dword (E8: byte) a lane to LDS at m0 + 4 lane.
 template <bool E8>
-__device__ __forceinline__ void dma_scale(i32x4_t rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
+__device__ __forceinline__ void dma_scale(i32x4_t rsrc, uint32_t voff) {
     if (E8)
-        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_ubyte %0, %1, %2 offen lds"
-                     :: "v"(voff), "s"(rsrc), "s"(soff), "s"(lds) : "memory", "m0");
+        asm volatile("buffer_load_ubyte %0, %1, 0 offen lds" :: "v"(voff), "s"(rsrc) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dword %0, %1, %2 offen lds"
-                     :: "v"(voff), "s"(rsrc), "s"(soff), "s"(lds) : "memory", "m0");
+        asm volatile("buffer_load_dword %0, %1, 0 offen lds" :: "v"(voff), "s"(rsrc) : "memory");
 }
 
 // One product from zero, into registers that a VALU instruction can read (the
@@ -72,13 +84,31 @@ __device__ __forceinline__ void accumulate(f32x4& d, const i32x8& b, const i32x8
 template <bool E8, bool TILED>
 struct Frag {
     i32x8 a[4], b[4];
-    float sa[4];
+    float sa[4], st;
     f32x4 sb[TILED || E8 ? 1 : 4];
     int ea[4], eb[4];
 };
 
+// Workgroups are dealt to the XCDs in turn: the one of each XCD's own range of
+// `n` pieces of work that workgroup b takes.
+__device__ __forceinline__ int xcd_order(int b, int n) {
+    const int x = b % kXcds, q = n / kXcds, r = n % kXcds;
+    return x * q + min(x, r) + b / kXcds;
+}
+
+// Tiles in groups of kGroup tile rows, down the columns of a group: the 32 tiles
+// that an XCD works on together then share eight tile rows of A and four of B
+// in its L2.
+constexpr int kGroup = 8;
+__device__ __forceinline__ void tile_of(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
+    const int group = uniform(t / (kGroup * tiles_n)), first = group * kGroup, rows = min(tiles_m - first, kGroup);
+    const int in = t - group * kGroup * tiles_n;
+    tn = uniform(in / rows);
+    tm = first + in - tn * rows;
+}
+
 template <int AF, bool E8, bool TILED, bool OUT_BF16>
-__global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, int KB, int tiles_n,
+__global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, int KB, int tiles_m, int tiles_n,
                                                           const uint8_t* __restrict__ A, const void* __restrict__ As,
                                                           const uint8_t* __restrict__ B, const void* __restrict__ Bs,
                                                           void* __restrict__ C, int parts, float* __restrict__ part) {
@@ -86,8 +116,10 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1, l16 = lane & 15, g = lane >> 4;
     // (divisions run in vector registers: back to scalars)
-    const int item = uniform((int)blockIdx.x / parts), p = (int)blockIdx.x - item * parts;
-    const int tm = uniform(item / tiles_n), tn = item - tm * tiles_n;
+    const int work = xcd_order((int)blockIdx.x, (int)gridDim.x), tiles = tiles_m * tiles_n;
+    const int p = uniform(work / tiles), item = work - p * tiles;
+    int tm, tn;
+    tile_of(item, tiles_m, tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * kTile, n0 = (int64_t)tn * kTile;
     const int kb0 = uniform(KB * p / parts), kb1 = uniform(KB * (p + 1) / parts);
     const uint32_t Kp = (uint32_t)KB * 128u;
@@ -98,52 +130,66 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
     const int64_t x0 = isA ? m0 : n0, rows = isA ? M : N, left = rows - x0;
     const i32x4_t src =
         buffer_rsrc((isA ? A : B) + x0 * Kp, (uint32_t)uniform((int)(left < kTile ? left : kTile)) * Kp);
-    const uint32_t voff = (uint32_t)(64 * (wave & 1) + (lane >> 3)) * Kp + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+    uint32_t voff[8];                                // of load i, less its immediate offset
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        voff[i] = (uint32_t)(64 * (wave & 1) + 8 * i + (lane >> 3)) * Kp + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16) -
+                  (uint32_t)((i & 3) * 1024);
     const uint32_t lds = lds_addr(sP) + (uint32_t)wave * 64u * kRowBytes, lds_s = lds_addr(sP) + kStage + wave * 256u;
     // scales of 64 rows of the wave's operand, one row of the array a stage; of
     // a tile, the one scale
     const bool tile_scale = TILED && !isA;
-    const int64_t sstep = (tile_scale ? 1 : scale_pitch(rows)) * kEl;
-    const uint8_t* const sbase = (const uint8_t*)(isA ? As : Bs) + (tile_scale ? (int64_t)tn * KB : x0) * kEl;
+    const uint64_t sstep = uniform64((uint64_t)((tile_scale ? 1 : scale_pitch(rows)) * kEl));
+    uint64_t sat = uniform64((uint64_t)(uintptr_t)(isA ? As : Bs) +       // of the stage that is loaded next
+                             (uint64_t)(tile_scale ? (int64_t)tn * KB + kb0 : kb0 * scale_pitch(rows) + x0) * kEl);
     const uint32_t srow = tile_scale ? 0u : (uint32_t)min((int64_t)(64 * (wave & 1) + lane), left - 1) * kEl;
-    // load i of stage kb: rows 8i .. 8i + 7, then the scales
+    // step i of stage kb's loads (rows 8i .. 8i + 7, at last the scales); m0 is
+    // written a step before the load that takes it
     auto load = [&](auto ic, int kb, int slot) {
         constexpr int i = decltype(ic)::value;
-        if constexpr (i < 8) {
-            dma_buf_x4<i * 1024>(src, voff + (uint32_t)kb * 128u + i * 8 * Kp, 0u, lds + (uint32_t)(slot * kStageAll));
-        } else {
-            dma_scale<E8>(buffer_rsrc(sbase + kb * sstep, kTile * kEl), srow, 0u, lds_s + (uint32_t)(slot * kStageAll));
+        if constexpr (i < 8) dma_rows<(i & 3) * 1024>(src, voff[i], (uint32_t)kb * 128u);
+        else {
+            dma_scale<E8>(i32x4_t{(int)(uint32_t)sat, (int)(uint32_t)(sat >> 32), (int)(kTile * kEl), 0x00020000}, srow);
+            sat += kb + 1 < kb1 ? sstep : 0;
         }
+        if constexpr (i == 3) set_m0(lds + (uint32_t)(slot * kStageAll) + 4096u);
+        if constexpr (i == 7) set_m0(lds_s + (uint32_t)(slot * kStageAll));
     };
     using F = Frag<E8, TILED>;
-    const uint8_t* const pa = sP + (wm * 64 + l16) * kRowBytes;
-    const uint8_t* const pb = sP + (kTile + wn * 64 + l16) * kRowBytes;
-    const int c0 = (g ^ (l16 & 7)) * 16, c1 = ((g + 4) ^ (l16 & 7)) * 16;
-    // half h of a lane's 32 bytes of row group i: chunks g and g + 4 of eight,
+    // Half h of a lane's 32 bytes of row group i: chunks g and g + 4 of eight,
     // which lie at their number XOR row % 8 (which k they are does not matter
-    // as long as both operands agree)
-    auto frag = [&](i32x8& f, const uint8_t* base, int i, int h, int slot) {
-        const uint4 v = *reinterpret_cast<const uint4*>(base + slot * kStageAll + i * 16 * kRowBytes + (h ? c1 : c0));
+    // as long as both operands agree).  Slots 0, 1 and 2, 3 have base pointers of
+    // their own: what is added to them fits the instructions' offsets.
+    const uint8_t* base[2][2][2];                    // [slot pair][operand][half]
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+            const int at = s2 * 2 * kStageAll + ((g + 4 * h) ^ (l16 & 7)) * 16 + l16 * kRowBytes;
+            base[s2][0][h] = sP + at + wm * 64 * kRowBytes;
+            base[s2][1][h] = sP + at + (kTile + wn * 64) * kRowBytes;
+        }
+    auto frag = [&](i32x8& f, int op, int i, int h, int slot) {
+        const uint4 v = *reinterpret_cast<const uint4*>(base[slot / 2][op][h] + (slot % 2) * kStageAll + i * 16 * kRowBytes);
         f[4 * h] = (int)v.x; f[4 * h + 1] = (int)v.y; f[4 * h + 2] = (int)v.z; f[4 * h + 3] = (int)v.w;
     };
+    const uint8_t* scales[2][2];                     // [slot pair][operand]
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+        scales[s2][0] = sP + s2 * 2 * kStageAll + kStage + wm * 256 + l16 * 4;
+        scales[s2][1] = sP + s2 * 2 * kStageAll + kStage + (2 + wn) * 256 + (TILED ? 0 : (E8 ? l16 : 4 * g) * 4);
+    }
     auto read_scales = [&](F& f, int slot) {
-        const uint8_t* const s = sP + slot * kStageAll + kStage;
+        const uint8_t* const a = scales[slot / 2][0] + (slot % 2) * kStageAll;
+        const uint8_t* const b = scales[slot / 2][1] + (slot % 2) * kStageAll;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint8_t* at = s + wm * 256 + (16 * i + l16) * 4;
-            if (E8) f.ea[i] = *reinterpret_cast<const int*>(at);
-            else f.sa[i] = *reinterpret_cast<const float*>(at);
-            if (E8) {
-                if (!TILED || i == 0) f.eb[i] = *reinterpret_cast<const int*>(s + (2 + wn) * 256 + (TILED ? 0 : 16 * i + l16) * 4);
-            } else if (!TILED) {
-                f.sb[i] = *reinterpret_cast<const f32x4*>(s + (2 + wn) * 256 + (16 * i + 4 * g) * 4);
-            }
+            if (E8) f.ea[i] = *reinterpret_cast<const int*>(a + i * 64);
+            else f.sa[i] = *reinterpret_cast<const float*>(a + i * 64);
+            if (E8 && (!TILED || i == 0)) f.eb[i] = *reinterpret_cast<const int*>(b + i * 64);
+            if (!E8 && !TILED) f.sb[i] = *reinterpret_cast<const f32x4*>(b + i * 64);
         }
-        if (TILED && !E8) {
-            const float t = *reinterpret_cast<const float*>(s + 2 * 256);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f.sa[i] *= t;
-        }
+        if (TILED && !E8) f.st = *reinterpret_cast<const float*>(b);
     };
 
     f32x4 acc[4][4];
@@ -157,6 +203,11 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
     // products later, when it has left the matrix pipe (at least 14 instructions
     // after its own, whatever else stands between them).
     auto turn = [&](F& f, F& n, int slot, int kb, int to) {
+        set_m0(lds + (uint32_t)(to * kStageAll));
+        if (TILED && !E8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.sa[i] *= f.st;
+        }
         f32x4 q[E8 ? 1 : 4];
         auto add = [&](auto xc) {
             constexpr int x = decltype(xc)::value, j = x / 4, i = x % 4;
@@ -173,7 +224,7 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
                 product<AF>(q[x % 4], f.b[j], f.a[i]);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (x < 9) load(xc, kb, to);
-            frag(x < 8 ? n.a[x / 2 % 4] : n.b[x / 2 % 4], x < 8 ? pa : pb, x / 2 % 4, x % 2, slot);
+            frag(x < 8 ? n.a[x / 2 % 4] : n.b[x / 2 % 4], x / 8, x / 2 % 4, x % 2, slot);
             if constexpr (!E8 && x >= 3) add(std::integral_constant<int, x - 3>{});
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -191,27 +242,37 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
     // waits count the same loads in every turn
     if (n > 0) {
 #pragma unroll
-        for (int k = 0; k < kRing; ++k)
-            static_for<0, kLoads>([&](auto ic) { load(ic, min(kb0 + k, kb1 - 1), k); });
+        for (int k = 0; k < kRing; ++k) {
+            set_m0(lds + (uint32_t)(k * kStageAll));
+            asm volatile("s_nop 0");
+            static_for<0, kLoads>([&](auto ic) {
+                load(ic, min(kb0 + k, kb1 - 1), k);
+                asm volatile("s_nop 0");
+            });
+        }
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads * (kRing - 1)) : "memory");
         F f, h;
         read_scales(f, 0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            frag(f.a[i / 2], pa, i / 2, i % 2, 0);
-            frag(f.b[i / 2], pb, i / 2, i % 2, 0);
+            frag(f.a[i / 2], 0, i / 2, i % 2, 0);
+            frag(f.b[i / 2], 1, i / 2, i % 2, 0);
         }
-        auto step = [&](F& cur, F& nxt, int k) {
+        auto step = [&](F& cur, F& nxt, int k, int slot) {
             // stage k + 1 has landed everywhere, every wave holds stage k
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads * (kRing - 2)) : "memory");
-            turn(cur, nxt, (k + 1) % kRing, min(kb0 + k + kRing, kb1 - 1), k % kRing);
+            turn(cur, nxt, (slot + 1) % kRing, min(kb0 + k + kRing, kb1 - 1), slot);
         };
         int k = 0;
-        for (; k + 1 < n; k += 2) {
-            step(f, h, k);
-            step(h, f, k + 1);
+        for (; k + 4 <= n; k += 4) {
+            step(f, h, k, 0);
+            step(h, f, k + 1, 1);
+            step(f, h, k + 2, 2);
+            step(h, f, k + 3, 3);
         }
-        if (k < n) step(f, h, k);
+        if (k < n) step(f, h, k, 0);
+        if (k + 1 < n) step(h, f, k + 1, 1);
+        if (k + 2 < n) step(f, h, k + 2, 2);
         // no load outlives the kernel's LDS, and the last products have landed
         asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
@@ -225,26 +286,60 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
             for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(out + (j * 4 + i) * 256) = acc[j][i];
         return;
     }
+    // The tile goes through LDS: a lane holds four columns of one row, and whole
+    // rows (256 or 512 bytes) make whole lines.
+    constexpr int kEs = OUT_BF16 ? 2 : 4, kPitch = kTile * kEs + 16, kPer = 16 / kEs;   // elements of a 16-byte piece
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + wm * 64 + 16 * i + l16;
-        if (m >= M) continue;
+        uint8_t* const at = sP + (wm * 64 + 16 * i + l16) * kPitch + (wn * 64 + 4 * g) * kEs;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) store4<OUT_BF16>(C, m, n0 + wn * 64 + 16 * j + 4 * g, N, acc[j][i]);
+        for (int j = 0; j < 4; ++j) {
+            if (OUT_BF16)
+                *reinterpret_cast<uint2*>(at + 16 * j * kEs) =
+                    make_uint2(pack_bf16x2(acc[j][i][0], acc[j][i][1]), pack_bf16x2(acc[j][i][2], acc[j][i][3]));
+            else
+                *reinterpret_cast<f32x4*>(at + 16 * j * kEs) = acc[j][i];
+        }
+    }
+    __syncthreads();
+    constexpr int kPieces = kTile / kPer;            // of a row
+    const int c = threadIdx.x % kPieces;
+    const int64_t col = n0 + c * kPer;
+    if (col >= N) return;
+#pragma unroll 4
+    for (int r = threadIdx.x / kPieces; r < kTile; r += 256 / kPieces) {
+        if (m0 + r >= M) break;
+        const uint4 v = *reinterpret_cast<const uint4*>(sP + r * kPitch + c * 16);
+        uint8_t* const d = (uint8_t*)C + ((m0 + r) * N + col) * kEs;
+        if (col + kPer <= N) {
+            __builtin_memcpy(d, &v, 16);
+        } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (col + e < N) {
+                    if (OUT_BF16) ((uint16_t*)d)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+                    else ((uint32_t*)d)[e] = w[e & 3];
+                }
+        }
     }
 }
 
 // The parts' sums of one sixteenth of a tile, in order.
 template <bool OUT_BF16>
-__global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(int64_t M, int64_t N, int64_t tiles_n, void* __restrict__ C,
-                                                           int parts, const float* __restrict__ part) {
+__global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(int64_t M, int64_t N, int tiles_m, int tiles_n,
+                                                           void* __restrict__ C, int parts,
+                                                           const float* __restrict__ part) {
     const int64_t item = blockIdx.x / 16;
+    int tm, tn;
+    tile_of((int)item, tiles_m, tiles_n, tm, tn);
     const int at = (blockIdx.x % 16) * 256 + threadIdx.x, lane = at & 63, ji = at >> 6 & 15, wave = at >> 10;
     const float* in = part + item * parts * (kTile * kTile) + at * 4;
     f32x4 v = *reinterpret_cast<const f32x4*>(in);
     for (int p = 1; p < parts; ++p) v += *reinterpret_cast<const f32x4*>(in + (int64_t)p * (kTile * kTile));
-    const int64_t m = item / tiles_n * kTile + (wave >> 1) * 64 + (ji & 3) * 16 + (lane & 15);
-    const int64_t n = item % tiles_n * kTile + (wave & 1) * 64 + (ji >> 2) * 16 + (lane >> 4) * 4;
+    const int64_t m = (int64_t)tm * kTile + (wave >> 1) * 64 + (ji & 3) * 16 + (lane & 15);
+    const int64_t n = (int64_t)tn * kTile + (wave & 1) * 64 + (ji >> 2) * 16 + (lane >> 4) * 4;
     if (m < M) store4<OUT_BF16>(C, m, n, N, v);
 }
 
@@ -270,12 +365,13 @@ hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, co
     }
     auto go = [&](auto af, auto e, auto tl, auto bf) {
         hipLaunchKernelGGL((gemm_fp8_kernel<decltype(af)::value, decltype(e)::value, decltype(tl)::value, decltype(bf)::value>),
-                           dim3((unsigned)(tm * tn * parts)), dim3(256), 0, s, M, N, (int)KB, (int)tn, a, as, b, bs, c,
+                           dim3((unsigned)(tm * tn * parts)), dim3(256), 0, s, M, N, (int)KB, (int)tm, (int)tn, a, as, b,
+                           bs, c,
                            (int)parts, part);
         hipError_t e2 = hipGetLastError();
         if (e2 != hipSuccess || parts == 1) return e2;
         hipLaunchKernelGGL((gemm_fp8_sum_kernel<decltype(bf)::value>), dim3((unsigned)(tm * tn * 16)), dim3(256), 0, s,
-                           M, N, tn, c, (int)parts, part);
+                           M, N, (int)tm, (int)tn, c, (int)parts, part);
         return hipGetLastError();
     };
     using Y = std::true_type;
