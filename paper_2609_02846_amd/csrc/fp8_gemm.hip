@@ -225,6 +225,10 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (x < 9) load(xc, kb, to);
             frag(x < 8 ? n.a[x / 2 % 4] : n.b[x / 2 % 4], x / 8, x / 2 % 4, x % 2, slot);
+            if constexpr (!E8 && x == 3) {           // no additions stand before this one
+                asm volatile("s_nop 5");
+                __builtin_amdgcn_sched_barrier(0);
+            }
             if constexpr (!E8 && x >= 3) add(std::integral_constant<int, x - 3>{});
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -345,6 +349,15 @@ __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(int64_t M, int64_t N,
 
 }  // namespace
 
+// Whether the 256 x 256 tiles take an E8M0 product faster: modelled times in
+// us, whole rounds of one tile a CU, each with a fixed part and one for each
+// block.  Model / measured (256 CUs): 8192 x 4096 x 21504 wide 555 / 534, small
+// 795 / 790; 2000 x 4096 x 4096 wide 63 / 56, small 41 / 38.
+static bool wide_is_faster(int64_t M, int64_t N, int64_t KB, int cus) {
+    auto rounds = [&](int64_t t) { return (double)(((M + t - 1) / t * ((N + t - 1) / t) + cus - 1) / cus); };
+    return KB > 0 && rounds(256) * (12.0 + 1.58 * KB) < rounds(128) * (2.0 + 0.58 * KB);
+}
+
 hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
                            const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16,
                            hipStream_t s) {
@@ -355,6 +368,8 @@ hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, co
     int cus = 0;
     hipError_t err = device_cus(&cus);
     if (err != hipSuccess) return err;
+    if (e8 && wide_is_faster(M, N, KB, cus))
+        return launch_gemm_fp8_wide(M, N, K, cus, a, as, a_fmt, b, bs, tiled, c, c_bf16, s);
     int64_t parts = std::min<int64_t>(cus / std::max<int64_t>(tm * tn, 1), KB / 8);
     if (parts < 1) parts = 1;
     Workspace held;                                  // until the sum is enqueued

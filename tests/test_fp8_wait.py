@@ -1,7 +1,8 @@
-"""The 8-bit GEMM of 128 x 128 tiles issues its products as instructions the
-compiler does not model, so it does not keep reads of their results clear of
-products still in the matrix pipe; the kernel's own order has to.  Checked on
-the built library, over straight-line code and over the loops' back edges."""
+"""The 8-bit GEMMs of 128 x 128 and 256 x 256 tiles issue their products as
+instructions the compiler does not model, so it does not keep accesses of their
+results clear of products still in the matrix pipe; the kernels' own order has
+to.  Checked on the built library, over straight-line code and over every
+branch."""
 
 import os
 import re
@@ -13,9 +14,9 @@ import paper_2609_02846_amd as ue
 from paper_2609_02846_amd import build as ue_build
 from test_mfma_wait import LLVM, _code_objects
 
-# v_mfma_f32_16x16x128_f8f6f4 on 8-bit operands takes 8 passes: a VALU, LDS or
-# memory instruction may touch its result after this many others.
-WAIT = 12
+# States after which a VALU, LDS or memory instruction may touch the result of a
+# product on 8-bit operands: of 8 passes (16 x 16 x 128) and 16 (32 x 32 x 64).
+WAIT = {"gemm_fp8_kernel": 12, "gemm_fp8_wide_kernel": 20}
 
 
 @pytest.fixture(scope="module")
@@ -24,7 +25,7 @@ def kernels(tmp_path_factory):
         ue_build.build(verbose=False)
     tmp, found = tmp_path_factory.mktemp("isa"), {}
     for i, obj in enumerate(_code_objects(ue.LIB_PATH)):
-        if b"gemm_fp8_kernel" not in obj:
+        if b"gemm_fp8_kernel" not in obj and b"gemm_fp8_wide_kernel" not in obj:
             continue
         f = tmp / f"{i}.o"
         f.write_bytes(obj)
@@ -33,7 +34,7 @@ def kernels(tmp_path_factory):
                                    check=True).stdout.splitlines():
             m = re.match(r"[0-9a-f]+ <(.+)>:$", line)
             if m:
-                name = m.group(1) if "gemm_fp8_kernel" in m.group(1) else None
+                name = m.group(1) if any(k + "I" in m.group(1) for k in WAIT) else None
                 if name:
                     found[name] = []
             elif name and "//" in line:
@@ -55,7 +56,7 @@ def _states(text):
     return int(m.group(1)) + 1 if m else 1
 
 
-def _walk(code, order):
+def _walk(code, order, wait, jump=None):
     """Instructions of ``order`` that touch a product's result too early."""
     pending, bad = [], []                        # (registers, states since)
     for i in order:
@@ -63,9 +64,11 @@ def _walk(code, order):
         mfma = text.startswith("v_mfma")
         regs = _registers(text)
         # a product may accumulate on another's result: the matrix pipe's own order
-        if not mfma and any(regs & r for r, n in pending if n < WAIT):
+        if not mfma and any(regs & r for r, n in pending if n < wait):
             bad.append(text)
-        pending = [(r, n + _states(text)) for r, n in pending if n < WAIT]
+        pending = [(r, n + _states(text)) for r, n in pending if n < wait]
+        if i != jump and text.startswith(("s_branch", "s_endpgm")):
+            pending = []                         # what follows in memory does not follow in time
         if mfma:
             dest = re.match(r"\S+ ([va]\[\d+:\d+\])", text).group(1)
             pending.append((_registers(dest), 0))
@@ -73,16 +76,18 @@ def _walk(code, order):
 
 
 def test_products_land_before_they_are_read(kernels):
-    assert len(kernels) == 16                    # two formats, scale kinds, tilings and outputs
+    # two formats, tilings and outputs; of the smaller tiles both scale kinds
+    assert sum("gemm_fp8_kernel" in n for n in kernels) == 16 and len(kernels) == 24
     for name, code in kernels.items():
+        wait = next(w for k, w in WAIT.items() if k + "I" in name)
         at = {a: i for i, (a, _) in enumerate(code)}
         assert sum(t.startswith("v_mfma") for _, t in code) >= 32, name
-        assert not any("scratch_" in t for _, t in code), name
-        assert _walk(code, range(len(code))) == [], name
-        # every backward branch: the loop's last instructions, then its first
+        assert _walk(code, range(len(code)), wait) == [], name
+        # every branch: the instructions before it, then those at its target
         for i, (a, text) in enumerate(code):
             m = re.match(r"s_c?branch\S* (\d+)", text)
-            if m and int(m.group(1)) >= 0x8000:
-                target = a + 4 + 4 * (int(m.group(1)) - 0x10000)
-                j = at[target]
-                assert _walk(code, list(range(max(0, i - 60), i + 1)) + list(range(j, min(j + 60, len(code))))) == [], name
+            if m:
+                offset = int(m.group(1))
+                j = at[a + 4 + 4 * (offset - 0x10000 if offset >= 0x8000 else offset)]
+                order = list(range(max(0, i - 60), i + 1)) + list(range(j, min(j + 60, len(code))))
+                assert _walk(code, order, wait, i) == [], name

@@ -230,6 +230,43 @@ def test_integer_products_are_exact():
             assert np.array_equal(c.cpu().numpy(), (A @ B.T).astype(np.float32)), (M, N, K, kind)
 
 
+# enough 256 x 256 tiles for the kernel of large products (one and several a
+# workgroup, ragged edges, odd and even numbers of blocks, one block)
+LARGE = [(2900, 2950, 384), (4100, 4200, 520), (2816, 3330, 100), (6000, 4097, 1290)]
+
+
+@pytest.mark.parametrize("tiled", [False, True])
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+def test_large_products(scale, tiled):
+    """Whole numbers (every output exact) under scales that are powers of two
+    and differ from row to row, and sampled outputs of random codes."""
+    rng = np.random.default_rng(11)
+    for M, N, K in LARGE:
+        say("gemm_fp8 large", scale, tiled, M, N, K)
+        kb = pad128(K) // 128
+        a = torch.randint(-4, 5, (M, pad128(K)), device="cuda").float()
+        b = torch.randint(-4, 5, (N, pad128(K)), device="cuda").float()
+        a[:, K:] = b[:, K:] = 0
+        ea = torch.randint(0, 4, (kb, scale_pitch(M)), device="cuda")
+        eb = torch.randint(0, 4, (pad128(N) // 128, kb) if tiled else (kb, scale_pitch(N)), device="cuda")
+        enc = (lambda e: torch.exp2(e.float())) if scale == "f32" else (lambda e: (e + 127).to(torch.uint8))
+        rows_b = eb.repeat_interleave(128, 0)[:N] if tiled else eb[:, :N].t()
+        wide = lambda v, e: (v.view(v.shape[0], kb, 128) * torch.exp2(e.float())[:, :, None]).view(v.shape)  # noqa: E731
+        want = wide(a, ea[:, :M].t()) @ wide(b, rows_b).t()      # below 2^24: exact in binary32
+        for fmt in ("e4m3", "e5m2"):
+            args = (a.to(FP8[fmt]), enc(ea).contiguous(), b.to(FP8["e4m3"]), enc(eb).contiguous())
+            blk = "tile" if tiled else "row"
+            guard = torch.full((M * N + 64,), 7.0, device="cuda")
+            c = ue.gemm_fp8("nt", M, N, K, *args, b_blk=blk, out=guard[:M * N].view(M, N))
+            assert torch.equal(c, want) and (guard[M * N:] == 7.0).all()
+            assert torch.equal(ue.gemm_fp8("nt", M, N, K, *args, b_blk=blk), want.to(torch.bfloat16))
+        ops = operands(M, N, K, scale, "e5m2", tiled, M)
+        c = ue.gemm_fp8("nt", M, N, K, *ops[:4], b_blk="tile" if tiled else "row", out_dtype=torch.float32)
+        m, n = (torch.from_numpy(rng.choice(v, 150, replace=False)).cuda() for v in (M, N))
+        product_check(c[m][:, n], (ops[4][0][m], ops[4][1][m], ops[4][2]), (ops[5][0][n], ops[5][1][n], ops[5][2]), K,
+                      f"{M} {N} {K}")
+
+
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 def test_bad_values_stay_in_their_row(scale):
     """A NaN token spoils its own outputs and nothing else."""
