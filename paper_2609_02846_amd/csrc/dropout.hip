@@ -31,18 +31,19 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, const
     const int64_t chunks = (n + 7) / 8, stride = (int64_t)gridDim.x * kDropThreads;
     for (int64_t j = (int64_t)blockIdx.x * kDropThreads + threadIdx.x; j < chunks; j += stride) {
         const Vec8<T> v = load8(x, 8 * j, n);
-        Vec8<T> r, o;
+        Vec8<T> r;
+        float o[8];
         if (RES) r = load8(res, 8 * j, n);
         const uint4 c = philox4x32_10(make_uint4((uint32_t)j, (uint32_t)((uint64_t)j >> 32), tensor_id, 1u), key0, key1);
         const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t bits = e % 2 ? w[e / 2] >> 16 : w[e / 2] & 0xFFFFu;
-            float f = bits >= drop ? (float)v.e[e] * up : 0.0f;
-            if (RES) f = (float)r.e[e] + f;
-            o.e[e] = (T)f;
+            float f = bits >= drop ? v.get(e) * up : 0.0f;
+            if (RES) f = r.get(e) + f;
+            o[e] = f;
         }
-        store8(y, 8 * j, n, o);
+        store8(y, 8 * j, n, Vec8<T>::of(o));
     }
 }
 

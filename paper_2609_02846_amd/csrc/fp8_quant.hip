@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict
         rmax[i] = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float a = finite_abs((float)v[i].e[j]);
+            const float a = finite_abs(v[i].get(j));
             rmax[i] = fmaxf(rmax[i], a);
             if (kCols) cmax[j] = fmaxf(cmax[j], a);
         }
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict
             if (r0 + i < R) {
                 float q[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = s.value((float)v[i].e[j]);
+                for (int j = 0; j < 8; ++j) q[j] = s.value(v[i].get(j));
                 const uint2 w = make_uint2(pack_fp8<E5M2>(q[0], q[1], q[2], q[3]), pack_fp8<E5M2>(q[4], q[5], q[6], q[7]));
                 *reinterpret_cast<uint2*>(out.rows + (r0 + i) * Cp + c0) = w;
                 if (kRows && cg == i) put_scale(out.rows_scale, bc * scale_pitch(R) + r0 + i, s);
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict
         }
         float q[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = s.value((float)v[i].e[j]);
+        for (int i = 0; i < 8; ++i) q[i] = s.value(v[i].get(j));
         *reinterpret_cast<uint2*>(sT + (cg * 8 + j) * 128 + ((rg ^ cg) & 15) * 8) =
             make_uint2(pack_fp8<E5M2>(q[0], q[1], q[2], q[3]), pack_fp8<E5M2>(q[4], q[5], q[6], q[7]));
     }
@@ -154,12 +154,12 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_rows_kernel(const T* __res
     const Vec8<T> v = load8(x + r * C, c, r < R ? C : 0);
     float a = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) a = fmaxf(a, finite_abs((float)v.e[j]));
+    for (int j = 0; j < 8; ++j) a = fmaxf(a, finite_abs(v.get(j)));
     const BlockScale<E8> s = BlockScale<E8>::of(row16_max(a), E5M2);
     if (r >= R) return;
     float q[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = s.value((float)v.e[j]);
+    for (int j = 0; j < 8; ++j) q[j] = s.value(v.get(j));
     *reinterpret_cast<uint2*>(out + r * (blocks_c * 128) + c) =
         make_uint2(pack_fp8<E5M2>(q[0], q[1], q[2], q[3]), pack_fp8<E5M2>(q[4], q[5], q[6], q[7]));
     if (t == 0) put_scale(scales, bc * scale_pitch(R) + r, s);

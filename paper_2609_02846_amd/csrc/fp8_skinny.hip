@@ -85,11 +85,11 @@ __global__ __launch_bounds__(64 * NW) void gemm_fp8_skinny_kernel(const SkinnyAr
             const Vec8<bf16> v = load8(x + (int64_t)t * g.K, k, g.K);
             float a = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a = fmaxf(a, finite_abs((float)v.e[e]));
+            for (int e = 0; e < 8; ++e) a = fmaxf(a, finite_abs(v.get(e)));
             const BlockScale<E8> s = BlockScale<E8>::of(row16_max(a), false);
             float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = s.value((float)v.e[e]);
+            for (int e = 0; e < 8; ++e) y[e] = s.value(v.get(e));
             *reinterpret_cast<uint2*>(dyn + t * row + k) =
                 make_uint2(pack_fp8<false>(y[0], y[1], y[2], y[3]), pack_fp8<false>(y[4], y[5], y[6], y[7]));
             if (l16 == 0) sA[t * KB + kb] = E8 ? (El)s.code() : (El)s.scale();

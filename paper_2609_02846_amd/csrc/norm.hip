@@ -38,7 +38,29 @@ __device__ __forceinline__ float row_sum(float v, float* red, int wave) {
     return s;
 }
 
-template <typename T, typename P, int NW, int U>
+// v, as values that the compiler knows nothing of.
+template <typename T>
+__device__ __forceinline__ void forget(Vec8<T>& v) {
+#pragma unroll
+    for (int i = 0; i < Vec8<T>::kWords; ++i) asm volatile("" : "+v"(v.w[i]));
+}
+
+// Rows by length: below eight elements (NW = U = 1), whole vectors of eight, any
+// other.
+enum class Len : int { Tiny, Whole, Ragged };
+
+template <Len L, typename T>
+__device__ __forceinline__ Vec8<T> row8(const T* row, int c, int C) {
+    if constexpr (L == Len::Tiny) return load8(row, c, C);
+    if constexpr (L == Len::Ragged) return load8_row(row, c, C);
+    Vec8<T> v;
+    __builtin_memcpy(&v, row + (c < C ? c : 0), sizeof v);
+#pragma unroll
+    for (int i = 0; i < Vec8<T>::kWords; ++i) v.w[i] = c < C ? v.w[i] : 0u;
+    return v;
+}
+
+template <typename T, typename P, int NW, int U, Len L>
 __global__ __launch_bounds__(NW > 4 ? 64 * NW : 256) void norm_fwd_kernel(const T* __restrict__ x,
                                                                           const P* __restrict__ w,
                                                                           const P* __restrict__ b, T* __restrict__ y,
@@ -47,30 +69,38 @@ __global__ __launch_bounds__(NW > 4 ? 64 * NW : 256) void norm_fwd_kernel(const 
                                                                           int C, float eps) {
     constexpr int kThreads = NW > 4 ? 64 * NW : 256, kRows = kThreads / 64 / NW;
     __shared__ float red[2][kThreads / 64];
-    const int wave = threadIdx.x >> 6, c0 = ((wave % NW) * 64 + (threadIdx.x & 63)) * 8;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c0 = ((wave % NW) * 64 + (threadIdx.x & 63)) * 8;
     const float inv = 1.0f / (float)C;
     // a workgroup's waves take the same number of turns (they share barriers)
     for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < rows; r0 += (int64_t)gridDim.x * kRows) {
-        const int64_t r = r0 + wave / NW;
-        const bool live = r < rows;
-        const T* xr = x + r * C;
+        const bool live = r0 + wave / NW < rows;
+        const int64_t r = live ? r0 + wave / NW : rows - 1;
         Vec8<T> v[U];
-        float sum = 0.0f;
+        Vec8<P> wv[U], bv[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            v[u] = load8(xr, c0 + u * NW * 512, live ? C : 0);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += (float)v[u].e[e];
+            const int c = c0 + u * NW * 512;
+            v[u] = row8<L>(x + r * C, c, C);
+            if (U <= 2 && w != nullptr) wv[u] = row8<L>(w, c, C);
+            if (U <= 2 && b != nullptr) bv[u] = row8<L>(b, c, C);
         }
-        const float mean = row_sum<NW>(sum, red[0], wave) * inv;
-        float sq = 0.0f;
+        float sum = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
+            for (int e = 0; e < 8; ++e) sum += v[u].get(e);
+        const float mean = row_sum<NW>(sum, red[0], wave) * inv;
+        float sq = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (U > 2) forget(v[u]);
+#pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = (float)v[u].e[e] - mean;
+                const float d = v[u].get(e) - mean;
                 sq += c0 + u * NW * 512 + e < C ? d * d : 0.0f;
             }
+            if (U > 2) __builtin_amdgcn_sched_barrier(0);
+        }
         const float rstd = 1.0f / sqrtf(row_sum<NW>(sq, red[1], wave) * inv + eps);
         if (!live) continue;
         if (c0 == 0) {
@@ -81,18 +111,21 @@ __global__ __launch_bounds__(NW > 4 ? 64 * NW : 256) void norm_fwd_kernel(const 
         for (int u = 0; u < U; ++u) {
             const int c = c0 + u * NW * 512;
             if (c >= C) break;
-            Vec8<P> wv, bv;
-            if (w != nullptr) wv = load8(w, c, C);
-            if (b != nullptr) bv = load8(b, c, C);
-            Vec8<T> o;
+            if (U > 2) {                             // (no registers for them before)
+                forget(v[u]);
+                if (w != nullptr) wv[u] = row8<L>(w, c, C);
+                if (b != nullptr) bv[u] = row8<L>(b, c, C);
+            }
+            float o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float h = ((float)v[u].e[e] - mean) * rstd;
-                if (w != nullptr) h *= (float)wv.e[e];
-                if (b != nullptr) h += (float)bv.e[e];
-                o.e[e] = (T)h;
+                float h = (v[u].get(e) - mean) * rstd;
+                if (w != nullptr) h *= wv[u].get(e);
+                if (b != nullptr) h += bv[u].get(e);
+                o[e] = h;
             }
-            store8(y + r * C, c, C, o);
+            store8(y + r * C, c, C, Vec8<T>::of(o));
+            if (U > 2) __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
@@ -105,7 +138,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const T* __restrict
                                                              float* __restrict__ mean_out, float* __restrict__ rstd_out,
                                                              int64_t rows, int64_t C, float eps) {
     __shared__ float red[2][16];
-    const int wave = threadIdx.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const float inv = 1.0f / (float)C;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T* xr = x + r * C;
@@ -113,7 +146,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const T* __restrict
         for (int64_t c = 8 * (int64_t)threadIdx.x; c < C; c += 8192) {
             const Vec8<T> v = load8(xr, c, C);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += (float)v.e[e];
+            for (int e = 0; e < 8; ++e) sum += v.get(e);
         }
         const float mean = row_sum<16>(sum, red[0], wave) * inv;
         float sq = 0.0f;
@@ -121,7 +154,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const T* __restrict
             const Vec8<T> v = load8(xr, c, C);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = (float)v.e[e] - mean;
+                const float d = v.get(e) - mean;
                 sq += c + e < C ? d * d : 0.0f;
             }
         }
@@ -135,22 +168,22 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const T* __restrict
             Vec8<P> wv, bv;
             if (w != nullptr) wv = load8(w, c, C);
             if (b != nullptr) bv = load8(b, c, C);
-            Vec8<T> o;
+            float o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float h = ((float)v.e[e] - mean) * rstd;
-                if (w != nullptr) h *= (float)wv.e[e];
-                if (b != nullptr) h += (float)bv.e[e];
-                o.e[e] = (T)h;
+                float h = (v.get(e) - mean) * rstd;
+                if (w != nullptr) h *= wv.get(e);
+                if (b != nullptr) h += bv.get(e);
+                o[e] = h;
             }
-            store8(y + r * C, c, C, o);
+            store8(y + r * C, c, C, Vec8<T>::of(o));
         }
     }
 }
 
 // One workgroup takes rows b, b + grid, ... in groups of kRows, writes dx and
 // keeps the column sums of dy h and dy; part: [grid][2][C].
-template <typename T, typename P, int NW, int U>
+template <typename T, typename P, int NW, int U, Len L>
 __global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const T* __restrict__ x, const T* __restrict__ dy,
                                                                const P* __restrict__ w, const float* __restrict__ mean,
                                                                const float* __restrict__ rstd,
@@ -159,7 +192,7 @@ __global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const T* __restri
     constexpr int kRows = kBwdThreads / 64 / NW;
     __shared__ float red[2][2][kBwdThreads / 64];
     __shared__ float col[kRows > 1 ? NW * 512 : 1];
-    const int wave = threadIdx.x >> 6, c0 = ((wave % NW) * 64 + (threadIdx.x & 63)) * 8;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c0 = ((wave % NW) * 64 + (threadIdx.x & 63)) * 8;
     const float inv = 1.0f / (float)C;
     float dw[U][8], db[U][8];
 #pragma unroll
@@ -168,31 +201,35 @@ __global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const T* __restri
         for (int e = 0; e < 8; ++e) dw[u][e] = db[u][e] = 0.0f;
     int turn = 0;
     for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < rows; r0 += (int64_t)gridDim.x * kRows, turn ^= 1) {
-        const int64_t r = r0 + wave / NW;
-        const bool live = r < rows;
-        const float mu = live ? mean[r] : 0.0f, rs = live ? rstd[r] : 0.0f;
-        Vec8<T> xv[U], gv[U];
+        const bool live = r0 + wave / NW < rows;
+        const int64_t r = live ? r0 + wave / NW : rows - 1;
+        const float mu = mean[r], rs = rstd[r];
+        Vec8<T> xv[U], gv[U], rv[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            xv[u] = load8(x + r * C, c0 + u * NW * 512, live ? C : 0);
-            gv[u] = load8(dy + r * C, c0 + u * NW * 512, live ? C : 0);
+            const int c = c0 + u * NW * 512;
+            xv[u] = row8<L>(x + r * C, c, C);
+            gv[u] = row8<L>(dy + r * C, c, C);
+            if (res != nullptr) rv[u] = row8<L>(res + r * C, c, C);
         }
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = c0 + u * NW * 512;
             Vec8<P> wv;
-            if (w != nullptr) wv = load8(w, c, C);
+            if (w != nullptr) wv = row8<L>(w, c, C);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                // past the row's end dy is 0 and x - mean is finite or the row's own
-                const float d = (float)gv[u].e[e], h = c + e < C && live ? ((float)xv[u].e[e] - mu) * rs : 0.0f;
-                const float g = w != nullptr ? d * (float)wv.e[e] : d;
+                // (past the row's end dy is 0, and so must h be: a NaN there would count)
+                const float d = live ? gv[u].get(e) : 0.0f;
+                const float h = c + e < C && live ? (xv[u].get(e) - mu) * rs : 0.0f;
+                const float g = w != nullptr ? d * wv.get(e) : d;
                 s1 += g;
                 s2 += g * h;
                 dw[u][e] += d * h;
                 db[u][e] += d;
             }
+            __builtin_amdgcn_sched_barrier(0);       // one vector's numbers at a time
         }
         s1 = wave_sum(s1);
         s2 = wave_sum(s2);
@@ -207,23 +244,30 @@ __global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const T* __restri
         s1 *= inv;
         s2 *= inv;
         if (!live || dx == nullptr) continue;
+        // the row is converted again from its 16-bit (or 32-bit) elements: kept as
+        // numbers since before the sums it takes more registers than there are
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            forget(xv[u]);
+            forget(gv[u]);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = c0 + u * NW * 512;
             if (c >= C) break;
             Vec8<P> wv;
-            if (w != nullptr) wv = load8(w, c, C);
-            Vec8<T> rv, o;
-            if (res != nullptr) rv = load8(res + r * C, c, C);
+            if (w != nullptr) wv = row8<L>(w, c, C);
+            float o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = (float)gv[u].e[e], h = ((float)xv[u].e[e] - mu) * rs;
-                const float g = w != nullptr ? d * (float)wv.e[e] : d;
+                const float d = gv[u].get(e), h = (xv[u].get(e) - mu) * rs;
+                const float g = w != nullptr ? d * wv.get(e) : d;
                 float v = (g - s1 - h * s2) * rs;
-                if (res != nullptr) v += (float)rv.e[e];
-                o.e[e] = (T)v;
+                if (res != nullptr) v += rv[u].get(e);
+                o[e] = v;
             }
-            store8(dx + r * C, c, C, o);
+            store8(dx + r * C, c, C, Vec8<T>::of(o));
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     if (part == nullptr) return;
@@ -260,7 +304,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const T* __restrict
                                                              const float* __restrict__ rstd, const T* __restrict__ res,
                                                              T* __restrict__ dx, int64_t rows, int64_t C) {
     __shared__ float red[2][16];
-    const int wave = threadIdx.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const float inv = 1.0f / (float)C;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const float mu = mean[r], rs = rstd[r];
@@ -271,9 +315,9 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const T* __restrict
             if (w != nullptr) wv = load8(w, c, C);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float g = (float)gv.e[e] * (w != nullptr ? (float)wv.e[e] : 1.0f);
+                const float g = gv.get(e) * (w != nullptr ? wv.get(e) : 1.0f);
                 s1 += g;
-                s2 += c + e < C ? g * (((float)xv.e[e] - mu) * rs) : 0.0f;
+                s2 += c + e < C ? g * ((xv.get(e) - mu) * rs) : 0.0f;
             }
         }
         s1 = row_sum<16>(s1, red[0], wave) * inv;
@@ -281,17 +325,18 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const T* __restrict
         for (int64_t c = 8 * (int64_t)threadIdx.x; c < C; c += 8192) {
             const Vec8<T> xv = load8(x + r * C, c, C), gv = load8(dy + r * C, c, C);
             Vec8<P> wv;
-            Vec8<T> rv, o;
+            Vec8<T> rv;
+            float o[8];
             if (w != nullptr) wv = load8(w, c, C);
             if (res != nullptr) rv = load8(res + r * C, c, C);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float g = (float)gv.e[e] * (w != nullptr ? (float)wv.e[e] : 1.0f);
-                float v = (g - s1 - ((float)xv.e[e] - mu) * rs * s2) * rs;
-                if (res != nullptr) v += (float)rv.e[e];
-                o.e[e] = (T)v;
+                const float g = gv.get(e) * (w != nullptr ? wv.get(e) : 1.0f);
+                float v = (g - s1 - (xv.get(e) - mu) * rs * s2) * rs;
+                if (res != nullptr) v += rv.get(e);
+                o[e] = v;
             }
-            store8(dx + r * C, c, C, o);
+            store8(dx + r * C, c, C, Vec8<T>::of(o));
         }
     }
 }
@@ -310,8 +355,8 @@ __global__ __launch_bounds__(64) void norm_cols_kernel(const T* __restrict__ x, 
         const Vec8<T> xv = load8(x + r * C, c, C), gv = load8(dy + r * C, c, C);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float d = (float)gv.e[e];
-            dw[e] += d * (((float)xv.e[e] - mu) * rs);
+            const float d = gv.get(e);
+            dw[e] += d * ((xv.get(e) - mu) * rs);
             db[e] += d;
         }
     }
@@ -356,22 +401,36 @@ hipError_t with_types(DType x, DType p, F&& f) {
     });
 }
 
-template <typename T, typename P, int NW, int U>
-hipError_t fwd(const T* x, int64_t rows, int64_t C, const P* w, const P* b, float eps, T* y, float* mean, float* rstd,
+template <typename T, typename P, int NW, int U, Len L>
+hipError_t fwd_l(const T* x, int64_t rows, int64_t C, const P* w, const P* b, float eps, T* y, float* mean, float* rstd,
                hipStream_t s) {
     constexpr int kThreads = NW > 4 ? 64 * NW : 256, kRows = kThreads / 64 / NW;
     const int64_t blocks = (rows + kRows - 1) / kRows;
-    hipLaunchKernelGGL((norm_fwd_kernel<T, P, NW, U>), dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))),
+    hipLaunchKernelGGL((norm_fwd_kernel<T, P, NW, U, L>), dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))),
                        dim3(kThreads), 0, s, x, w, b, y, mean, rstd, rows, (int)C, eps);
     return hipGetLastError();
+}
+
+template <typename T, typename P, int NW, int U, Len L>
+hipError_t bwd_l(const T* x, const T* dy, int64_t rows, int64_t C, const P* w, const float* mean, const float* rstd,
+               const T* res, T* dx, float* part, int blocks, hipStream_t s) {
+    hipLaunchKernelGGL((norm_bwd_kernel<T, P, NW, U, L>), dim3((unsigned)blocks), dim3(kBwdThreads), 0, s, x, dy, w, mean,
+                       rstd, res, dx, part, rows, (int)C);
+    return hipGetLastError();
+}
+
+template <typename T, typename P, int NW, int U>
+hipError_t fwd(const T* x, int64_t rows, int64_t C, const P* w, const P* b, float eps, T* y, float* mean, float* rstd,
+               hipStream_t s) {
+    return C % 8 == 0 ? fwd_l<T, P, NW, U, Len::Whole>(x, rows, C, w, b, eps, y, mean, rstd, s)
+                      : fwd_l<T, P, NW, U, Len::Ragged>(x, rows, C, w, b, eps, y, mean, rstd, s);
 }
 
 template <typename T, typename P, int NW, int U>
 hipError_t bwd(const T* x, const T* dy, int64_t rows, int64_t C, const P* w, const float* mean, const float* rstd,
                const T* res, T* dx, float* part, int blocks, hipStream_t s) {
-    hipLaunchKernelGGL((norm_bwd_kernel<T, P, NW, U>), dim3((unsigned)blocks), dim3(kBwdThreads), 0, s, x, dy, w, mean,
-                       rstd, res, dx, part, rows, (int)C);
-    return hipGetLastError();
+    return C % 8 == 0 ? bwd_l<T, P, NW, U, Len::Whole>(x, dy, rows, C, w, mean, rstd, res, dx, part, blocks, s)
+                      : bwd_l<T, P, NW, U, Len::Ragged>(x, dy, rows, C, w, mean, rstd, res, dx, part, blocks, s);
 }
 
 }  // namespace
@@ -384,6 +443,7 @@ hipError_t launch_norm(DType type, const void* x_, int64_t rows, int64_t C, DTyp
         const T* x = (const T*)x_;
         const P *w = (const P*)w_, *b = (const P*)b_;
         T* y = (T*)y_;
+        if (C < 8) return fwd_l<T, P, 1, 1, Len::Tiny>(x, rows, C, w, b, eps, y, mean, rstd, s);
         if (C <= 512) return fwd<T, P, 1, 1>(x, rows, C, w, b, eps, y, mean, rstd, s);
         if (C <= 1024) return fwd<T, P, 1, 2>(x, rows, C, w, b, eps, y, mean, rstd, s);
         if (C <= 2048) return fwd<T, P, 4, 1>(x, rows, C, w, b, eps, y, mean, rstd, s);
@@ -408,7 +468,7 @@ hipError_t launch_norm_grad(DType type, const void* x_, const void* dy_, int64_t
         T* dx = (T*)dx_;
         const bool sums = dw != nullptr || db != nullptr;
         // waves a row, and how many workgroups of 1024 threads take the rows
-        const int nw = C <= 512 ? 1 : C <= 1024 ? 2 : C <= 2048 ? 4 : C <= 4096 ? 4 : C <= 8192 ? 8 : 16;
+        const int nw = C <= 512 ? 1 : C <= 1024 ? 2 : C <= 2048 ? 4 : C <= 4096 ? 8 : 16;
         const int64_t groups = (rows + 16 / nw - 1) / (16 / nw);
         int parts = (int)(groups < kMaxParts ? groups : kMaxParts);
         if (C > kRegCols) parts = (int)(rows < 64 ? rows : 64);
@@ -418,11 +478,12 @@ hipError_t launch_norm_grad(DType type, const void* x_, const void* dy_, int64_t
         hipError_t e = hipSuccess;
         if (sums) e = held.take(kWsNorm, s, (size_t)parts * 2 * (size_t)C * sizeof(float), (void**)&part);
         if (e != hipSuccess) return e;
-        if (C <= 512) e = bwd<T, P, 1, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        if (C < 8) e = bwd_l<T, P, 1, 1, Len::Tiny>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= 512) e = bwd<T, P, 1, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
         else if (C <= 1024) e = bwd<T, P, 2, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
         else if (C <= 2048) e = bwd<T, P, 4, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
-        else if (C <= 4096) e = bwd<T, P, 4, 2>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
-        else if (C <= 8192) e = bwd<T, P, 8, 2>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= 4096) e = bwd<T, P, 8, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= 8192) e = bwd<T, P, 16, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
         else if (C <= 16384) e = bwd<T, P, 16, 2>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
         else if (C <= kRegCols) e = bwd<T, P, 16, 3>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
         else {
