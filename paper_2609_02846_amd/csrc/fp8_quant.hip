@@ -57,8 +57,17 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict
     const int64_t Cp = blocks_c * 128, Rp = (R + 127) / 128 * 128;
 
     Vec8<T> v[8];
+    if (C >= 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = load8(x + (r0 + i) * C, c0, r0 + i < R ? C : 0);
+        for (int i = 0; i < 8; ++i) v[i] = load8_row(x + min(r0 + i, R - 1) * C, (int)c0, (int)C);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int k = 0; k < Vec8<T>::kWords; ++k) v[i].w[k] = r0 + i < R ? v[i].w[k] : 0u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = load8(x + (r0 + i) * C, c0, r0 + i < R ? C : 0);
+    }
 
     float rmax[8], cmax[8] = {};
 #pragma unroll

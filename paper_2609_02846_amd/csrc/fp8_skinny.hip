@@ -39,7 +39,7 @@ __device__ __forceinline__ i32x8 load32(const uint8_t* p) {
 
 template <int NW, int MT, int AF, bool E8, bool TILED, bool FUSED, bool OUT_BF16>
 __global__ __launch_bounds__(64 * NW) void gemm_fp8_skinny_kernel(const SkinnyArgs g) {
-    constexpr int kU = MT > 2 ? 2 : 4;           // blocks in flight
+    constexpr int kU = MT > 2 ? 2 : 4;           // blocks of a turn, all loaded before the first is used
     __shared__ __attribute__((aligned(16))) f32x4 sums[NW][MT][64];
     extern __shared__ __attribute__((aligned(16))) uint8_t dyn[];    // FUSED: payload rows, then scales
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -75,6 +75,16 @@ __global__ __launch_bounds__(64 * NW) void gemm_fp8_skinny_kernel(const SkinnyAr
     };
 
     Block f[kU];
+    i32x8 a[FUSED ? 1 : kU][MT];                 // FUSED: read from LDS at the product
+    El sa[FUSED ? 1 : kU][MT];
+    auto fetch_a = [&](int u, int kb) {
+        kb = min(kb, KB - 1);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            a[u][t] = load32(arow[t] + (int64_t)kb * 128);
+            sa[u][t] = FUSED ? sA[at[t] * KB + kb] : as[kb * pa + at[t]];
+        }
+    };
 #pragma unroll
     for (int u = 0; u < kU; ++u) fetch(f[u], wave + u * NW);
 
@@ -101,27 +111,34 @@ __global__ __launch_bounds__(64 * NW) void gemm_fp8_skinny_kernel(const SkinnyAr
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     for (int k0 = wave; k0 < KB; k0 += kU * NW) {
+        if (!FUSED)
+#pragma unroll
+            for (int u = 0; u < kU; ++u) fetch_a(u, k0 + u * NW);
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             const int kb = k0 + u * NW;
             if (kb >= KB) break;
             const Block w = f[u];
-            if (kb + kU * NW < KB) fetch(f[u], kb + kU * NW);
+            if (FUSED) fetch_a(0, kb);
+            constexpr int kStep = FUSED ? 0 : 1;
+            const int v = u * kStep;
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
-                const i32x8 a = load32(arow[t] + (int64_t)kb * 128);
-                const El sa = FUSED ? sA[at[t] * KB + kb] : as[kb * pa + at[t]];
                 if (E8) {
-                    acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.w, a, acc[t], 0, AF, 0, (int)w.s, 0, (int)sa);
+                    acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.w, a[v][t], acc[t], 0, AF, 0, (int)w.s, 0,
+                                                                             (int)sa[v][t]);
                 } else {
                     const f32x4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        w.w, a, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, AF, 0, 0, 0, 0);
+                        w.w, a[v][t], f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, AF, 0, 0, 0, 0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        acc[t][e] = __builtin_fmaf(p[e], (float)sa * (TILED ? (float)w.s : w.s4[e]), acc[t][e]);
+                        acc[t][e] = __builtin_fmaf(p[e], (float)sa[v][t] * (TILED ? (float)w.s : w.s4[e]), acc[t][e]);
                 }
             }
         }
+        if (k0 + kU * NW < KB)
+#pragma unroll
+            for (int u = 0; u < kU; ++u) fetch(f[u], k0 + (kU + u) * NW);
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) sums[wave][t][lane] = acc[t];

@@ -379,8 +379,14 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict_
     P* const out = blockIdx.y == 0 ? dw : db;
     if (out == nullptr) return;
     float v = 0.0f;
-    if (c < C)
-        for (int i = wave; i < n; i += 16) v += part[((int64_t)i * 2 + blockIdx.y) * C + c];
+    const float* const in = part + (int64_t)blockIdx.y * C + (c < C ? c : 0);
+    for (int i = wave; i < n; i += 128) {            // eight loads in flight
+        float t[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = in[(int64_t)min(i + 16 * k, n - 1) * 2 * C];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += i + 16 * k < n ? t[k] : 0.0f;
+    }
     s[wave][lane] = v;
     __syncthreads();
     if (wave != 0 || c >= C) return;
