@@ -362,12 +362,12 @@ hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, co
                            const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16,
                            hipStream_t s) {
     const int64_t KB = (K + 127) / 128, tm = (M + kTile - 1) / kTile, tn = (N + kTile - 1) / kTile;
-    if (fp8_skinny(M, K)) return launch_gemm_fp8_skinny(M, N, K, a, as, a_fmt, b, bs, tiled, e8, c, c_bf16, s);
     // split along K while that still gives every CU at most one part of at
     // least eight stages
     int cus = 0;
     hipError_t err = device_cus(&cus);
     if (err != hipSuccess) return err;
+    if (fp8_skinny(M, K)) return launch_gemm_fp8_skinny(M, N, K, cus, a, as, a_fmt, b, bs, tiled, e8, c, c_bf16, s);
     if (e8 && wide_is_faster(M, N, KB, cus))
         return launch_gemm_fp8_wide(M, N, K, cus, a, as, a_fmt, b, bs, tiled, c, c_bf16, s);
     int64_t parts = std::min<int64_t>(cus / std::max<int64_t>(tm * tn, 1), KB / 8);

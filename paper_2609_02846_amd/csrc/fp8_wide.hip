@@ -232,8 +232,6 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_nop 4" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        int fresh = 0;
-        asm volatile("" : "+s"(fresh));              // (known to be 0, the loop's first turn becomes code of its own)
         for (int kb = 0; kb < KB; ++kb) {
             // slice 0 of this stage, its slice 1 read in between
             static_for<0, 16>([&](auto qc) {
@@ -243,10 +241,9 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
                 __builtin_amdgcn_sched_barrier(0);
             });
             // every wave has read this stage, the next one has landed
-            // (all but the one load ahead; after an epilogue's stores, which may
-            // leave out of turn, all)
-            if (kb == fresh) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            else asm volatile("s_waitcnt vmcnt(1) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            // (all but the one load ahead: loads come in order, and stores that are
+            // still out only make this wait longer)
+            asm volatile("s_waitcnt vmcnt(1) lgkmcnt(0)\n\ts_barrier" ::: "memory");
             const int bn = b ^ 1;
             advance();
             start(b);

@@ -201,7 +201,7 @@ hipError_t launch_gemm_fp8_wide(int64_t M, int64_t N, int64_t K, int cus, const 
 // The same for few rows (whether it takes them: fp8_skinny), and with bf16
 // tokens that the kernel quantizes itself (fp8_fused).
 bool fp8_skinny(int64_t M, int64_t K);
-hipError_t launch_gemm_fp8_skinny(int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
+hipError_t launch_gemm_fp8_skinny(int64_t M, int64_t N, int64_t K, int cus, const uint8_t* a, const void* as, Fp8 a_fmt,
                                   const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16,
                                   hipStream_t s);
 bool fp8_fused(int64_t T, int64_t K);
