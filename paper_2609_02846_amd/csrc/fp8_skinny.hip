@@ -257,8 +257,11 @@ hipError_t launch(const SkinnyArgs& g, int cus, bool e5m2, bool tiled, bool e8, 
                 return hipGetLastError();
             };
             auto waves = [&](auto m, auto af, auto tl) {
-                if constexpr (FUSED || decltype(m)::value == 1) return go(std::integral_constant<int, 8>{}, m, af, tl);
-                else return go(std::integral_constant<int, 4>{}, m, af, tl);
+                // four waves, so that a CU holds two workgroups of 16 rows of A; eight
+                // where there is not a tile for every CU
+                if constexpr (decltype(m)::value == 1)
+                    if (tiles <= cus) return go(std::integral_constant<int, 8>{}, m, af, tl);
+                return go(std::integral_constant<int, 4>{}, m, af, tl);
             };
             if constexpr (FUSED) {
                 return waves(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, Y{});
