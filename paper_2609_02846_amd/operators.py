@@ -43,7 +43,10 @@ def scale_pitch(n):
 def _on(stream):
     """Outputs of a call on ``stream`` are that stream's memory, as torch's
     allocator counts it."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _tensor(t, name, dtypes, like=None, dim=None):
@@ -54,14 +57,14 @@ def _tensor(t, name, dtypes, like=None, dim=None):
         raise ValueError(f"{name} must be a contiguous CUDA/HIP tensor of {names}")
     if dim is not None and t.dim() != dim:
         raise ValueError(f"{name} must have {dim} dimensions, not {t.dim()}")
-    if t.device.index != (torch._C._cuda_getDevice() if like is None else like.device.index):
+    if t.get_device() != (torch._C._cuda_getDevice() if like is None else like.get_device()):
         raise ValueError(f"{name} is on {t.device}, not on the device of the call")
     return t
 
 
 def _like(t, x, name):
     """``t`` (or None) with the shape, type and device of ``x``."""
-    if t is not None and (_tensor(t, name, (x.dtype,), x).shape != x.shape):
+    if t is not None and _tensor(t, name, (x.dtype,), x).shape != x.shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(x.shape)} needed")
     return t
 
@@ -82,16 +85,21 @@ def _affine(x, weight, bias):
     return _TYPES[x.dtype if dtype is None else dtype]
 
 
+def norm_args(x, weight, bias):
+    """Checks; element type code of the parameters, rows and columns."""
+    _tensor(x, "x", _TYPES)
+    if x.dim() == 0:
+        raise ValueError("x must have a dimension to normalise")
+    C = x.shape[-1]
+    return _affine(x, weight, bias), x.numel() // C if C else 0, C
+
+
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, stats=False, out=None, stream=None):
     """Layer norm over the last dimension of ``x`` (bf16, fp16 or fp32; see
     ue5m3_layer_norm).  ``weight`` and ``bias``: of x's type or fp32, or None.
     Returns y, with ``stats`` (y, mean, rstd): the fp32 statistics of the rows,
     which ``layer_norm_grad`` takes."""
-    _tensor(x, "x", tuple(_TYPES))
-    if x.dim() == 0:
-        raise ValueError("x must have a dimension to normalise")
-    pt, C = _affine(x, weight, bias), x.shape[-1]
-    rows = x.numel() // C if C else 0
+    pt, rows, C = norm_args(x, weight, bias)
     with _on(stream):
         y = torch.empty_like(x) if out is None else _like(out, x, "out")
         mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device) if stats else (None, None)
@@ -106,7 +114,7 @@ def layer_norm_grad(x, dy, weight, mean, rstd, residual_grad=None, need=(True, T
     dweight, dbias), each None where ``need`` says so.  ``residual_grad`` is
     added to dx.  dweight and dbias have the type of ``weight``, or
     ``param_dtype`` where that is None."""
-    _tensor(x, "x", tuple(_TYPES))
+    _tensor(x, "x", _TYPES)
     _like(dy, x, "dy")
     _like(residual_grad, x, "residual_grad")
     pt, C = _affine(x, weight, None), x.shape[-1]
@@ -133,7 +141,7 @@ def dropout_forward(x, p, seed, tensor_id=0, residual=None, out=None, stream=Non
     """[residual +] dropout of ``x`` (bf16, fp16 or fp32) with the mask of
     (seed, tensor_id) (see ue5m3_dropout).  The same call on a gradient is
     the backward pass.  ``out`` may be ``x`` or ``residual``."""
-    _tensor(x, "x", tuple(_TYPES))
+    _tensor(x, "x", _TYPES)
     _like(residual, x, "residual")
     with _on(stream):
         y = torch.empty_like(x) if out is None else _like(out, x, "out")
@@ -169,7 +177,7 @@ def quantize_fp8(x, axis, fmt="e4m3", scale="e8m0", stream=None):
     """Quantizes ``x`` [R, C] (bf16, fp16 or fp32) in blocks of 128 along its
     rows (axis 1) or down its columns (axis 0, stored transposed); see
     ue5m3_quantize_fp8.  Returns (payload, scales)."""
-    _tensor(x, "x", tuple(_TYPES), dim=2)
+    _tensor(x, "x", _TYPES, dim=2)
     _formats(fmt, scale)
     if axis not in (0, 1):
         raise ValueError("axis must be 0 or 1")
@@ -183,7 +191,7 @@ def quantize_fp8(x, axis, fmt="e4m3", scale="e8m0", stream=None):
 def quantize_fp8_dual(x, fmt="e4m3", scale="e8m0", stream=None):
     """Both blockings of ``x`` from one read: ((payload, scales) of axis 1,
     (payload, scales) of axis 0), as ``quantize_fp8`` gives them."""
-    _tensor(x, "x", tuple(_TYPES), dim=2)
+    _tensor(x, "x", _TYPES, dim=2)
     _formats(fmt, scale)
     R, C = x.shape
     with _on(stream):
@@ -196,7 +204,7 @@ def quantize_fp8_tiles(w, scale="e8m0", transposed=True, stream=None):
     """Quantizes a weight ``w`` [R, C] to E4M3 in 128 x 128 tiles (see
     ue5m3_quantize_fp8_tiles).  Returns (payload, scales, payload_t, scales_t),
     the last two None unless ``transposed``."""
-    _tensor(w, "w", tuple(_TYPES), dim=2)
+    _tensor(w, "w", _TYPES, dim=2)
     _formats("e4m3", scale)
     R, C = w.shape
     rb, cb = pad128(R) // 128, pad128(C) // 128
@@ -215,7 +223,7 @@ def quantize_fp8_tiles(w, scale="e8m0", transposed=True, stream=None):
 def _operand(p, s, rows, K, tiled, dtypes, name):
     """An 8-bit operand: ``rows`` payload rows over a contraction of K."""
     _tensor(p, name, dtypes)
-    _tensor(s, name + "_scales", tuple(_SCALE_CODES))
+    _tensor(s, name + "_scales", _SCALE_CODES)
     _dev_buf(p, p.dtype, rows * pad128(K), name)
     blocks = pad128(K) // 128
     _dev_buf(s, s.dtype, blocks * (pad128(rows) // 128 if tiled else scale_pitch(rows)), name + "_scales")
@@ -233,7 +241,7 @@ def gemm_fp8(layout, M, N, K, a, a_scales, b, b_scales, out=None, out_dtype=torc
     a_blk = ("colT" if lay == TN else "row") if a_blk is None else a_blk
     b_blk = ("colT" if lay == TN else "tile") if b_blk is None else b_blk
     if M > 0 and N > 0 and K > 0:
-        _operand(a, a_scales, M, K, False, tuple(_FP8_CODES), "a")
+        _operand(a, a_scales, M, K, False, _FP8_CODES, "a")
         _operand(b, b_scales, N, K, b_blk == "tile", (torch.float8_e4m3fn,), "b")
         if a_scales.dtype != b_scales.dtype:
             raise ValueError("the scales of both operands must be of one kind")
@@ -257,7 +265,7 @@ def linear_fp8(x, w, w_scales, out=None, out_dtype=torch.bfloat16, stream=None):
     ue5m3_linear_fp8.  Returns [..., N]."""
     _tensor(x, "x", (torch.bfloat16,))
     _tensor(w, "w", (torch.float8_e4m3fn,), x, 2)
-    _tensor(w_scales, "w_scales", tuple(_SCALE_CODES), x, 2)
+    _tensor(w_scales, "w_scales", _SCALE_CODES, x, 2)
     K, N = x.shape[-1], w.shape[0]
     T = x.numel() // K if K else _numel(x.shape[:-1])
     if w.shape[1] != pad128(K) or w_scales.shape != (pad128(N) // 128, pad128(K) // 128):

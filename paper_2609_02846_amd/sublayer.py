@@ -10,31 +10,52 @@ separate calls, and the results are theirs.
 import torch
 from torch.autograd.function import once_differentiable
 
+from . import _check, _stream, load_library
 from .dropout import Dropout
 from .fp8 import Fp8Linear, _check_formats, _flat, backward_products, forward_product
 from .norm import LayerNorm
-from .operators import dropout_forward, layer_norm_forward, layer_norm_grad
+from .operators import BF16, dropout_forward, layer_norm_forward, norm_args
 
 
 class _SublayerFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gain, bias, w, p, seed, tensor_id, eps, scale, grad_fmt, need_w):
-        h, mean, rstd = layer_norm_forward(x, gain, bias, eps, stats=True)
+        pt, T, C = norm_args(x, gain, bias)
+        lib, stream = load_library(), _stream()
+        h, stats = torch.empty_like(x), torch.empty(2 * T, dtype=torch.float32, device=x.device)
+        mean = stats.data_ptr()
+        _check(lib.ue5m3_layer_norm(x.data_ptr(), T, C, BF16, None if gain is None else gain.data_ptr(),
+                                    None if bias is None else bias.data_ptr(), pt, eps, h.data_ptr(), mean, mean + 4 * T,
+                                    stream), "ue5m3_layer_norm")
         y, keep = forward_product(h, w, scale, True, need_w)
-        ctx.save_for_backward(x, gain, mean, rstd, keep)
-        ctx.args = (*x.shape, w.shape[0], scale, grad_fmt, True, need_w)
-        ctx.key, ctx.param_dtype = (p, seed, tensor_id), None if bias is None else bias.dtype
-        return dropout_forward(y, p, seed, tensor_id, residual=x, out=y)
+        _check(lib.ue5m3_dropout(y.data_ptr(), T * C, BF16, p, seed, tensor_id, x.data_ptr(), y.data_ptr(), stream),
+               "ue5m3_dropout")
+        ctx.save_for_backward(x, gain, stats, keep)
+        ctx.args = (T, C, C, scale, grad_fmt, True, need_w)
+        ctx.key, ctx.pt = (p, seed, tensor_id), pt
+        return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
-        x, gain, mean, rstd, keep = ctx.saved_tensors
+        x, gain, stats, keep = ctx.saved_tensors
+        need_x, need_g, need_b = ctx.needs_input_grad[:3]
+        T, C = ctx.args[:2]
+        lib, stream = load_library(), _stream()
         dout = dout.to(torch.bfloat16).contiguous()
-        dh, dw = backward_products(dropout_forward(dout, *ctx.key), keep, *ctx.args)
-        dx, dgain, dbias = layer_norm_grad(x, dh, gain, mean, rstd, residual_grad=dout,
-                                           need=ctx.needs_input_grad[:3], param_dtype=ctx.param_dtype)
-        return dx, dgain, dbias, dw, None, None, None, None, None, None, None
+        dy, dev = torch.empty_like(dout), x.device
+        _check(lib.ue5m3_dropout(dout.data_ptr(), T * C, BF16, *ctx.key, None, dy.data_ptr(), stream), "ue5m3_dropout")
+        dh, dw = backward_products(dy, keep, *ctx.args)
+        pdtype = torch.bfloat16 if ctx.pt == BF16 else torch.float32
+        dx = dy if need_x else None                  # dropout's gradient has been read
+        dg = torch.empty(C, dtype=pdtype, device=dev) if need_g else None
+        db = torch.empty(C, dtype=pdtype, device=dev) if need_b else None
+        mean = stats.data_ptr()
+        _check(lib.ue5m3_layer_norm_grad(x.data_ptr(), dh.data_ptr(), T, C, BF16, None if gain is None else gain.data_ptr(),
+                                         ctx.pt, mean, mean + 4 * T, dout.data_ptr(), dx.data_ptr() if need_x else None,
+                                         dg.data_ptr() if need_g else None, db.data_ptr() if need_b else None, stream),
+               "ue5m3_layer_norm_grad")
+        return dx, dg, db, dw, None, None, None, None, None, None, None
 
 
 def sublayer(x, gain, bias, weight, p=0.1, seed=0, tensor_id=0, eps=1e-5, scale="e8m0", grad_fmt="e4m3"):
@@ -45,15 +66,14 @@ def sublayer(x, gain, bias, weight, p=0.1, seed=0, tensor_id=0, eps=1e-5, scale=
     if tuple(weight.shape) != (C, C):
         raise ValueError(f"the branch's weight must be [{C}, {C}] to add to its input")
     x2 = _flat(x, C)
-    grad = torch.is_grad_enabled()
-    if grad and any(t is not None and t.requires_grad for t in (x, gain, bias, weight)):
-        y = _SublayerFn.apply(x2, gain, bias, weight, float(p), int(seed), int(tensor_id), float(eps), scale, grad_fmt,
-                              weight.requires_grad)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, gain, bias, weight)):
+        y = _SublayerFn.apply(x2, gain, bias, weight, float(p), int(seed) & (2 ** 64 - 1), int(tensor_id) & 0xFFFFFFFF,
+                              float(eps), scale, grad_fmt, weight.requires_grad)
     else:
         h = layer_norm_forward(x2, gain, bias, eps)
         y, _ = forward_product(h, weight, scale, False, False)
         y = dropout_forward(y, p, seed, tensor_id, residual=x2, out=y)
-    return y.reshape(x.shape)
+    return y if x.dim() == 2 else y.reshape(x.shape)
 
 
 class PreNormSublayer(torch.nn.Module):
