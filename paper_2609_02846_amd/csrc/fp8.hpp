@@ -61,6 +61,13 @@ struct BlockScale<true> {                            // E8M0: powers of two
     __device__ __forceinline__ float value(float x) const { return __builtin_fmaf(x, 0.0f, x * inv); }
     __device__ __forceinline__ uint32_t code() const { return c; }
     __device__ __forceinline__ float scale() const { return __uint_as_float(c << 23); }
+    // What value() takes, as four numbers, and back.
+    __device__ __forceinline__ float4 pack() const { return make_float4(inv, 0.0f, 0.0f, 0.0f); }
+    __device__ __forceinline__ static BlockScale unpack(const float4& v) {
+        BlockScale s;
+        s.inv = v.x;
+        return s;
+    }
 };
 
 template <>
@@ -86,6 +93,14 @@ struct BlockScale<false> {                           // binary32
     }
     __device__ __forceinline__ uint32_t code() const { return 0; }
     __device__ __forceinline__ float scale() const { return s; }
+    __device__ __forceinline__ float4 pack() const { return make_float4(f, a, ra, 0.0f); }
+    __device__ __forceinline__ static BlockScale unpack(const float4& v) {
+        BlockScale s;
+        s.f = v.x;
+        s.a = v.y;
+        s.ra = v.z;
+        return s;
+    }
 };
 
 // Four values, at most the format's largest (up to the last binary32 bit),

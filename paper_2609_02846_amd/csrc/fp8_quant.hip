@@ -49,7 +49,8 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict
                                                              int64_t blocks_c, QuantOut out) {
     constexpr bool kRows = F == Form::Dual, kCols = F == Form::Cols || F == Form::Dual;
     constexpr bool kTiles = F == Form::Tiles || F == Form::TilesT, kT = kCols || F == Form::TilesT;
-    __shared__ float smax[4][128];
+    __shared__ float smax[5][128];                   // columns of the four waves, rows
+    __shared__ float4 sPar[kCols ? 2 : 1][kTiles ? 1 : 128];   // what rows and columns are divided by
     __shared__ __attribute__((aligned(16))) uint8_t sT[kT ? 128 * 128 : 16];
     const int t = threadIdx.x, cg = t & 15, rg = t >> 4, wave = t >> 6;
     const int64_t br = (int64_t)blockIdx.x / blocks_c, bc = (int64_t)blockIdx.x % blocks_c;
@@ -97,22 +98,16 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict
             if (kT) put_scale(out.cols_scale, bc * (Rp / 128) + br, tile);
         }
     }
-    if (kRows || kTiles) {
+    if (!kTiles) {
+        // One thread works out the scale of each row and of each column (a
+        // division or two: too dear for every thread to do its sixteen).
+        if (kRows) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const BlockScale<E8> s = kTiles ? tile : BlockScale<E8>::of(row16_max(rmax[i]), E5M2);
-            if (r0 + i < R) {
-                float q[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = s.value(v[i].get(j));
-                const uint2 w = make_uint2(pack_fp8<E5M2>(q[0], q[1], q[2], q[3]), pack_fp8<E5M2>(q[4], q[5], q[6], q[7]));
-                *reinterpret_cast<uint2*>(out.rows + (r0 + i) * Cp + c0) = w;
-                if (kRows && cg == i) put_scale(out.rows_scale, bc * scale_pitch(R) + r0 + i, s);
+            for (int i = 0; i < 8; ++i) {
+                const float a = row16_max(rmax[i]);
+                if (cg == i) smax[4][rg * 8 + i] = a;
             }
         }
-    }
-    if (!kT) return;
-    if (kCols) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float a = cmax[j];
@@ -124,15 +119,40 @@ __global__ __launch_bounds__(kThreads) void quant_fp8_kernel(const T* __restrict
             for (int j = 0; j < 8; ++j) smax[wave][cg * 8 + j] = cmax[j];
         }
         __syncthreads();
+        const int i = t & 127;
+        if (t < 128) {
+            const BlockScale<E8> s =
+                BlockScale<E8>::of(fmaxf(fmaxf(smax[0][i], smax[1][i]), fmaxf(smax[2][i], smax[3][i])), E5M2);
+            sPar[0][i] = s.pack();
+            if (bc * 128 + i < C) put_scale(out.cols_scale, br * scale_pitch(C) + bc * 128 + i, s);
+        } else if (kRows) {
+            const BlockScale<E8> s = BlockScale<E8>::of(smax[4][i], E5M2);
+            sPar[kCols ? 1 : 0][i] = s.pack();
+            if (br * 128 + i < R) put_scale(out.rows_scale, bc * scale_pitch(R) + br * 128 + i, s);
+        }
+        __syncthreads();
     }
+    if (kRows || kTiles) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            forget(v[i]);
+            const BlockScale<E8> s = kTiles ? tile : BlockScale<E8>::unpack(sPar[kCols ? 1 : 0][kTiles ? 0 : rg * 8 + i]);
+            if (r0 + i < R) {
+                float q[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[j] = s.value(v[i].get(j));
+                const uint2 w = make_uint2(pack_fp8<E5M2>(q[0], q[1], q[2], q[3]), pack_fp8<E5M2>(q[4], q[5], q[6], q[7]));
+                *reinterpret_cast<uint2*>(out.rows + (r0 + i) * Cp + c0) = w;
+            }
+        }
+    }
+    if (!kT) return;
+    // (converted again: kept as numbers the tile takes twice the registers)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) forget(v[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        BlockScale<E8> s = tile;
-        if (kCols) {
-            const int c = cg * 8 + j;
-            s = BlockScale<E8>::of(fmaxf(fmaxf(smax[0][c], smax[1][c]), fmaxf(smax[2][c], smax[3][c])), E5M2);
-            if (rg == j && c0 + j < C) put_scale(out.cols_scale, br * scale_pitch(C) + c0 + j, s);
-        }
+        const BlockScale<E8> s = kTiles ? tile : BlockScale<E8>::unpack(sPar[0][kTiles ? 0 : cg * 8 + j]);
         float q[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) q[i] = s.value(v[i].get(j));

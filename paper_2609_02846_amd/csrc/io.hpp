@@ -110,6 +110,13 @@ __device__ __forceinline__ void store8(T* p, int64_t i, int64_t n, const Vec8<T>
     }
 }
 
+// v, as values that the compiler knows nothing of.
+template <typename T>
+__device__ __forceinline__ void forget(Vec8<T>& v) {
+#pragma unroll
+    for (int i = 0; i < Vec8<T>::kWords; ++i) asm volatile("" : "+v"(v.w[i]));
+}
+
 // Sum over the 64 lanes, in every lane.
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll

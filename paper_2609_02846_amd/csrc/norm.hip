@@ -38,13 +38,6 @@ __device__ __forceinline__ float row_sum(float v, float* red, int wave) {
     return s;
 }
 
-// v, as values that the compiler knows nothing of.
-template <typename T>
-__device__ __forceinline__ void forget(Vec8<T>& v) {
-#pragma unroll
-    for (int i = 0; i < Vec8<T>::kWords; ++i) asm volatile("" : "+v"(v.w[i]));
-}
-
 // Rows by length: below eight elements (NW = U = 1), whole vectors of eight, any
 // other.
 enum class Len : int { Tiny, Whole, Ragged };
