@@ -213,6 +213,9 @@ __global__ __launch_bounds__(64 * NW) void gemm_fp8_skinny_kernel(const SkinnyAr
                 }
             }
         }
+        // The last product may be read 12 states after its issue; across the loop's
+        // branch the compiler leaves five.
+        if (E8) asm volatile("s_nop 11" ::: "memory");
 #pragma unroll
         for (int t = 0; t < MT; ++t) sums[(wave * MT + t) * 64 + lane] = acc[t];
         __syncthreads();

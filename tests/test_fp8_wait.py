@@ -1,8 +1,10 @@
 """The 8-bit GEMMs of 128 x 128 and 256 x 256 tiles issue their products as
 instructions the compiler does not model, so it does not keep accesses of their
 results clear of products still in the matrix pipe; the kernels' own order has
-to.  Checked on the built library, over straight-line code and over every
-branch."""
+to.  The kernel for few rows uses the compiler's own products, and where a
+branch lay between a product and the store of its result that compiler left too
+few states.  Checked on the built library, over straight-line code and over
+every branch."""
 
 import os
 import re
@@ -16,7 +18,7 @@ from test_mfma_wait import LLVM, _code_objects
 
 # States after which a VALU, LDS or memory instruction may touch the result of a
 # product on 8-bit operands: of 8 passes (16 x 16 x 128) and 16 (32 x 32 x 64).
-WAIT = {"gemm_fp8_kernel": 12, "gemm_fp8_wide_kernel": 20}
+WAIT = {"gemm_fp8_kernel": 12, "gemm_fp8_wide_kernel": 20, "gemm_fp8_skinny_kernel": 12}
 
 
 @pytest.fixture(scope="module")
@@ -25,7 +27,7 @@ def kernels(tmp_path_factory):
         ue_build.build(verbose=False)
     tmp, found = tmp_path_factory.mktemp("isa"), {}
     for i, obj in enumerate(_code_objects(ue.LIB_PATH)):
-        if b"gemm_fp8_kernel" not in obj and b"gemm_fp8_wide_kernel" not in obj:
+        if not any(k.encode() in obj for k in WAIT):
             continue
         f = tmp / f"{i}.o"
         f.write_bytes(obj)
@@ -77,11 +79,11 @@ def _walk(code, order, wait, jump=None):
 
 def test_products_land_before_they_are_read(kernels):
     # two formats, tilings and outputs; of the smaller tiles both scale kinds
-    assert sum("gemm_fp8_kernel" in n for n in kernels) == 16 and len(kernels) == 24
+    assert sum("gemm_fp8_kernel" in n for n in kernels) == 16 and len(kernels) > 24
     for name, code in kernels.items():
         wait = next(w for k, w in WAIT.items() if k + "I" in name)
         at = {a: i for i, (a, _) in enumerate(code)}
-        assert sum(t.startswith("v_mfma") for _, t in code) >= 32, name
+        assert sum(t.startswith("v_mfma") for _, t in code) >= (1 if "skinny" in name else 32), name
         assert _walk(code, range(len(code)), wait) == [], name
         # every branch: the instructions before it, then those at its target
         for i, (a, text) in enumerate(code):

@@ -268,6 +268,22 @@ def test_large_products(scale, tiled):
 
 
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("M,N,K,tiled", [(1, 21504, 130, True), (1, 9000, 520, False), (20, 20011, 257, True),
+                                         (40, 9001, 1024, False), (64, 12345, 384, True)])
+def test_few_rows_by_many_columns(M, N, K, tiled, scale):
+    """Several groups of B's rows for each workgroup, and a last round that
+    leaves some of them idle."""
+    say("few rows", M, N, K, tiled, scale)
+    a, sa, b, sb, A, B = operands(M, N, K, scale, "e4m3", tiled, N)
+    c = ue.gemm_fp8("nt", M, N, K, a, sa, b, sb, b_blk="tile" if tiled else "row", out_dtype=torch.float32)
+    product_check(c, A, B, K, f"{M} {N} {K}")
+    if tiled and M * pad128(K) <= 16384:              # quantized where it is multiplied
+        x = tensor(M, K, N)
+        A = quantized(x.double().cpu().numpy(), "e4m3", scale)
+        product_check(ue.linear_fp8(x, b, sb, out_dtype=torch.float32), A, B, K, f"serve {M} {N} {K}")
+
+
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
 def test_bad_values_stay_in_their_row(scale):
     """A NaN token spoils its own outputs and nothing else."""
     for T in (3, 20, 140):
