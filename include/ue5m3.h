@@ -16,10 +16,10 @@
  *   allocates and frees them.  Every pointer must be 16-byte aligned.  The
  *   only memory the library allocates itself is a set of workspaces, one of
  *   each kind per (device, stream): the split-tile partials of ue5m3_gemm,
- *   the expanded block-32 scales of ue5m3_gemm_ex / ue5m3_gemm_pm, and
- *   16 KiB of per-workgroup partial maxima for the amax calls, the column
- *   sums of ue5m3_layer_norm_grad and the quantized tokens of
- *   ue5m3_linear_fp8.  A workspace
+ *   the expanded block-32 scales of ue5m3_gemm_ex / ue5m3_gemm_pm, 16 KiB of
+ *   per-workgroup partial maxima for the amax calls, the column sums of
+ *   ue5m3_layer_norm_grad, the split-tile partials of ue5m3_gemm_fp8, and the
+ *   quantized tokens and split-tile partials of ue5m3_linear_fp8.  A workspace
  *   is allocated (hipMalloc) by the first call on that pair that needs it,
  *   or needs a larger one; a replaced workspace is never freed before the
  *   process ends, so work already enqueued or captured in a graph keeps a

@@ -358,26 +358,41 @@ static bool wide_is_faster(int64_t M, int64_t N, int64_t KB, int cus) {
     return KB > 0 && rounds(256) * (12.0 + 1.58 * KB) < rounds(128) * (2.0 + 0.58 * KB);
 }
 
-hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
-                           const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16,
-                           hipStream_t s) {
-    const int64_t KB = (K + 127) / 128, tm = (M + kTile - 1) / kTile, tn = (N + kTile - 1) / kTile;
-    // split along K while that still gives every CU at most one part of at
-    // least eight stages
+// Which kernel takes the product, and in how many parts along K the 128 x 128
+// tiles take it: as many as give every CU at most one part of at least eight
+// stages.  bytes: what the parts' partial sums take.
+struct Plan {
+    enum { Skinny, Wide, Tiles } kernel = Tiles;
     int cus = 0;
-    hipError_t err = device_cus(&cus);
+    int64_t tm = 0, tn = 0, parts = 1;
+    size_t bytes = 0;
+};
+
+static hipError_t make_plan(int64_t M, int64_t N, int64_t K, bool e8, Plan& p) {
+    hipError_t err = device_cus(&p.cus);
     if (err != hipSuccess) return err;
-    if (fp8_skinny(M, K)) return launch_gemm_fp8_skinny(M, N, K, cus, a, as, a_fmt, b, bs, tiled, e8, c, c_bf16, s);
-    if (e8 && wide_is_faster(M, N, KB, cus))
-        return launch_gemm_fp8_wide(M, N, K, cus, a, as, a_fmt, b, bs, tiled, c, c_bf16, s);
-    int64_t parts = std::min<int64_t>(cus / std::max<int64_t>(tm * tn, 1), KB / 8);
-    if (parts < 1) parts = 1;
-    Workspace held;                                  // until the sum is enqueued
-    float* part = nullptr;
-    if (parts > 1) {
-        err = held.take(kWsFp8, s, (size_t)(tm * tn * parts) * kTile * kTile * 4, (void**)&part);
-        if (err != hipSuccess) return err;
+    const int64_t KB = (K + 127) / 128;
+    p.tm = (M + kTile - 1) / kTile, p.tn = (N + kTile - 1) / kTile;
+    if (fp8_skinny(M, K)) {
+        p.kernel = Plan::Skinny;
+    } else if (e8 && wide_is_faster(M, N, KB, p.cus)) {
+        p.kernel = Plan::Wide;
+    } else {
+        p.parts = std::max<int64_t>(std::min<int64_t>(p.cus / std::max<int64_t>(p.tm * p.tn, 1), KB / 8), 1);
+        if (p.parts > 1) p.bytes = (size_t)(p.tm * p.tn * p.parts) * kTile * kTile * 4;
     }
+    return hipSuccess;
+}
+
+// part: p.bytes of workspace
+static hipError_t run_plan(const Plan& p, int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
+                           const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16, float* part,
+                           hipStream_t s) {
+    if (p.kernel == Plan::Skinny)
+        return launch_gemm_fp8_skinny(M, N, K, p.cus, a, as, a_fmt, b, bs, tiled, e8, c, c_bf16, s);
+    if (p.kernel == Plan::Wide)
+        return launch_gemm_fp8_wide(M, N, K, p.cus, a, as, a_fmt, b, bs, tiled, c, c_bf16, s);
+    const int64_t KB = (K + 127) / 128, tm = p.tm, tn = p.tn, parts = p.parts;
     auto go = [&](auto af, auto e, auto tl, auto bf) {
         hipLaunchKernelGGL((gemm_fp8_kernel<decltype(af)::value, decltype(e)::value, decltype(tl)::value, decltype(bf)::value>),
                            dim3((unsigned)(tm * tn * parts)), dim3(256), 0, s, M, N, (int)KB, (int)tm, (int)tn, a, as, b,
@@ -399,21 +414,35 @@ hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, co
     });
 }
 
+hipError_t launch_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* a, const void* as, Fp8 a_fmt,
+                           const uint8_t* b, const void* bs, bool tiled, bool e8, void* c, bool c_bf16,
+                           hipStream_t s) {
+    Plan p;
+    Workspace held;                                  // until the sum is enqueued
+    void* part = nullptr;
+    hipError_t e = make_plan(M, N, K, e8, p);
+    if (e == hipSuccess && p.bytes > 0) e = held.take(kWsFp8, s, p.bytes, &part);
+    if (e != hipSuccess) return e;
+    return run_plan(p, M, N, K, a, as, a_fmt, b, bs, tiled, e8, c, c_bf16, (float*)part, s);
+}
+
+// One workspace holds the parts' sums, the payload and the scales, so that
+// nothing is enqueued unless all of it is there.
 hipError_t launch_linear_fp8(const void* x, int64_t T, int64_t K, int64_t N, const uint8_t* w, const void* ws,
                              bool e8, void* y, bool y_bf16, hipStream_t s) {
     if (fp8_fused(T, K)) return launch_linear_fp8_fused(x, T, K, N, w, ws, e8, y, y_bf16, s);
     const int64_t KB = (K + 127) / 128;
     const size_t payload = (size_t)(T * KB * 128), scales = (size_t)(KB * scale_pitch(T)) * (e8 ? 1 : 4);
+    Plan p;
     Workspace held;                                  // until the product is enqueued
-    uint8_t* q = nullptr;
-    hipError_t e = hipSuccess;
-    if (K > 0) {
-        e = held.take(kWsTokens, s, payload + scales, (void**)&q);
-        if (e == hipSuccess)
-            e = launch_quant_fp8(DType::BF16, Fp8::E4M3, e8, x, T, K, q, q + payload, nullptr, nullptr, s);
-        if (e != hipSuccess) return e;
-    }
-    return launch_gemm_fp8(T, N, K, q, q + payload, Fp8::E4M3, w, ws, true, e8, y, y_bf16, s);
+    uint8_t* base = nullptr;
+    hipError_t e = make_plan(T, N, K, e8, p);
+    if (e == hipSuccess && K > 0) e = held.take(kWsTokens, s, p.bytes + payload + scales, (void**)&base);
+    if (e != hipSuccess) return e;
+    uint8_t* q = base + p.bytes;
+    if (K > 0) e = launch_quant_fp8(DType::BF16, Fp8::E4M3, e8, x, T, K, q, q + payload, nullptr, nullptr, s);
+    if (e != hipSuccess) return e;
+    return run_plan(p, T, N, K, q, q + payload, Fp8::E4M3, w, ws, true, e8, y, y_bf16, (float*)base, s);
 }
 
 }  // namespace ue5m3

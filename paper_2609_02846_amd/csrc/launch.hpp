@@ -27,8 +27,8 @@ enum class Fp8 : int { E4M3 = 0, E5M2 = 1 };
 // not freed, until the process ends): split-tile partials of the GEMMs,
 // block-32 scales expanded to the block-16 layout, per-workgroup partial
 // maxima of the amax kernels, per-workgroup column sums of layer norm's
-// backward pass, the quantized tokens of a serving call, split partials of the
-// 8-bit products.
+// backward pass, what a serving call in 8 bits keeps (its quantized tokens and
+// split partials), split partials of the other 8-bit products.
 enum WorkspaceKind : int { kWsSplit = 0, kWsScales = 1, kWsAmax = 2, kWsNorm = 3, kWsTokens = 4, kWsFp8 = 5, kWsKinds = 6 };
 
 // One call's use of a workspace.  Uses on one stream are ordered by the
@@ -36,7 +36,8 @@ enum WorkspaceKind : int { kWsSplit = 0, kWsScales = 1, kWsAmax = 2, kWsNorm = 3
 // workspace is held, against other host threads on the same stream, from
 // take() to the end of this object's life: keep it until the last launch
 // that touches the buffer is enqueued.  A call that needs several kinds takes
-// them in the order kWsScales, kWsSplit.  take() returns
+// them in the order kWsScales, kWsSplit; the kinds after kWsSplit are each
+// the only one that a call takes.  take() returns
 // hipErrorStreamCaptureUnsupported when s is capturing and an allocation
 // would be needed.
 struct WorkspaceSlot;

@@ -140,6 +140,17 @@ struct Call {
         void* const s = reinterpret_cast<void*>(stream);
         if (what == "amax")
             return sym<int (*)(const void*, int64_t, void*, int, void*)>("ue5m3_amax_accumulate")(f, M, f, 1, s);
+        if (what == "norm")
+            return sym<int (*)(const void*, const void*, int64_t, int64_t, int, const void*, int, const void*, const void*,
+                               const void*, void*, void*, void*, void*)>("ue5m3_layer_norm_grad")(
+                f, f, M, N, kind, f, 0, f, f, nullptr, f, f, f, s);
+        if (what == "fp8" && entry == "linear")
+            return sym<int (*)(const void*, int64_t, int64_t, int64_t, const void*, const void*, int, void*, int, void*)>(
+                "ue5m3_linear_fp8")(f, M, K, N, f, f, kind, f, out, s);
+        if (what == "fp8")
+            return sym<int (*)(int, int64_t, int64_t, int64_t, const void*, const void*, int, int, const void*,
+                               const void*, int, int, void*, int, void*)>("ue5m3_gemm_fp8")(
+                0, M, N, K, f, f, a_blk, 0, f, f, b_blk, kind, f, out, s);
         if (entry == "ex")
             return sym<int (*)(int, int64_t, int64_t, int64_t, void*, void*, int, void*, void*, void*, int, void*, void*,
                                int, int, void*)>("ue5m3_gemm_ex")(layout, M, N, K, f, f, a_blk, f, f, f, b_blk, f, f,
@@ -157,7 +168,8 @@ struct Call {
 bool parse(std::istream& in, Call& c) {
     if (!(in >> c.what)) return false;
     if (c.what == "amax") return (bool)(in >> c.M >> c.stream >> c.capturing);
-    return c.what == "gemm" && (bool)(in >> c.entry >> c.layout >> c.M >> c.N >> c.K >> c.a_blk >> c.b_blk >> c.out >>
+    if (c.what == "norm") return (bool)(in >> c.M >> c.N >> c.kind >> c.stream >> c.capturing);
+    return (c.what == "gemm" || c.what == "fp8") && (bool)(in >> c.entry >> c.layout >> c.M >> c.N >> c.K >> c.a_blk >> c.b_blk >> c.out >>
                                       c.kind >> c.stream >> c.capturing);
 }
 }  // namespace

@@ -51,6 +51,17 @@ def amax_call(numel, stream=0, capturing=False):
     return f"amax {numel} {stream} {int(capturing)}"
 
 
+def fp8_call(M, N, K, entry="gemm", out="bf16", scale="f32", tiled=True, stream=0, capturing=False):
+    """Command of one product in 8 bits ("gemm"), or of a serving call of M
+    tokens ("linear")."""
+    return (f"fp8 {entry} 0 {M} {N} {K} 6 {8 if tiled else 6} {1 if out == 'bf16' else 0} {int(scale == 'e8m0')} {stream} "
+            f"{int(capturing)}")
+
+
+def norm_grad_call(rows, cols, dtype=0, stream=0, capturing=False):
+    return f"norm {rows} {cols} {dtype} {stream} {int(capturing)}"
+
+
 def launches(calls):
     """Per call: (status, [(kernel with template arguments, grid, block), ...]).
     One process runs all of them in order (workspaces persist)."""
