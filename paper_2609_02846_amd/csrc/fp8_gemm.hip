@@ -25,16 +25,22 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
     return (uint64_t)(uint32_t)uniform((int)(uint32_t)(v >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)v);
 }
 
-constexpr int kTile = 128, kRowBytes = 128, kStage = 2 * kTile * kRowBytes;
+constexpr int kTile = 128, kRowBytes = 128;
 
-// 128 x 128 output tiles, four waves of 64 x 64, a ring of kRing stages of one
-// block each.  While a wave multiplies a stage out of registers it reads the
-// next one from LDS, and the stages after that are on their way: at the barrier
-// that opens turn k, stage k + 1 has landed and stage k has left the LDS, so
-// stage k + kRing takes its place.  Scales travel with their stage, one dword
+// Output tiles of 64 WM x 128, 2 WM waves of 64 x 64 (WM = 2 or 4), a ring of
+// stages of one block each.  While a wave multiplies a stage out of registers it
+// reads the next one from LDS, and the stages after that are on their way: at the
+// barrier that opens turn k, stage k + 1 has landed and stage k has left the LDS,
+// so stage k + kRing takes its place.  Scales travel with their stage, one dword
 // for each row (an E8M0 byte is loaded as one).
-constexpr int kRing = 4, kScaleBytes = 4 * 256, kStageAll = kStage + kScaleBytes;
-constexpr int kLoads = 9;                            // of a wave for one stage: 8 of rows, 1 of scales
+template <int WM>
+struct Tile {
+    static constexpr int kM = 64 * WM, kThreads = 128 * WM, kRing = WM == 2 ? 4 : 3;
+    static constexpr int kStage = (kM + kTile) * kRowBytes, kStageAll = kStage + 2 * WM * 256;
+    static constexpr int kLoadsB = 8 / WM;           // of a wave for one stage: rows of A 4, of B, scales 1
+    static constexpr int kLoads = 5 + kLoadsB;
+    static constexpr int kGroup = WM == 2 ? 8 : 4;   // tile rows, see tile_of()
+};
 
 // Direct loads to LDS that cost one instruction each: m0 holds the LDS address,
 // and the immediate offset counts for both sides (so a lane's source offset is
@@ -80,12 +86,11 @@ __device__ __forceinline__ void accumulate(f32x4& d, const i32x8& b, const i32x8
 }
 
 // Registers of one stage: a lane's share of 64 rows of each operand, and their
-// scales (E8: codes; else sa of each A row and, for 1D, sb of four rows).
+// scales (E8: codes; else sa of each A row and, tiled, the tile's).
 template <bool E8, bool TILED>
 struct Frag {
     i32x8 a[4], b[4];
     float sa[4], st;
-    f32x4 sb[TILED || E8 ? 1 : 4];
     int ea[4], eb[4];
 };
 
@@ -96,22 +101,23 @@ __device__ __forceinline__ int xcd_order(int b, int n) {
     return x * q + min(x, r) + b / kXcds;
 }
 
-// Tiles in groups of kGroup tile rows, down the columns of a group: the 32 tiles
-// that an XCD works on together then share eight tile rows of A and four of B
-// in its L2.
-constexpr int kGroup = 8;
-__device__ __forceinline__ void tile_of(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
-    const int group = uniform(t / (kGroup * tiles_n)), first = group * kGroup, rows = min(tiles_m - first, kGroup);
-    const int in = t - group * kGroup * tiles_n;
+// Tiles in groups of `height` tile rows, down the columns of a group: the 32 tiles
+// that an XCD works on together then share 1024 rows of A and 512 or 1024 of B in
+// its L2.
+__device__ __forceinline__ void tile_of(int t, int height, int tiles_m, int tiles_n, int& tm, int& tn) {
+    const int group = uniform(t / (height * tiles_n)), first = group * height, rows = min(tiles_m - first, height);
+    const int in = t - group * height * tiles_n;
     tn = uniform(in / rows);
     tm = first + in - tn * rows;
 }
 
-template <int AF, bool E8, bool TILED, bool OUT_BF16>
-__global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, int KB, int tiles_m, int tiles_n,
+template <int WM, int AF, bool E8, bool TILED, bool OUT_BF16>
+__global__ __launch_bounds__(128 * WM, 1) void gemm_fp8_kernel(int64_t M, int64_t N, int KB, int tiles_m, int tiles_n,
                                                           const uint8_t* __restrict__ A, const void* __restrict__ As,
                                                           const uint8_t* __restrict__ B, const void* __restrict__ Bs,
                                                           void* __restrict__ C, int parts, float* __restrict__ part) {
+    using L = Tile<WM>;
+    constexpr int kRing = L::kRing, kStage = L::kStage, kStageAll = L::kStageAll, kLoads = L::kLoads;
     __shared__ __attribute__((aligned(16))) uint8_t sP[kRing * kStageAll];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1, l16 = lane & 15, g = lane >> 4;
@@ -119,41 +125,43 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
     const int work = xcd_order((int)blockIdx.x, (int)gridDim.x), tiles = tiles_m * tiles_n;
     const int p = uniform(work / tiles), item = work - p * tiles;
     int tm, tn;
-    tile_of(item, tiles_m, tiles_n, tm, tn);
-    const int64_t m0 = (int64_t)tm * kTile, n0 = (int64_t)tn * kTile;
+    tile_of(item, L::kGroup, tiles_m, tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * L::kM, n0 = (int64_t)tn * kTile;
     const int kb0 = uniform(KB * p / parts), kb1 = uniform(KB * (p + 1) / parts);
     const uint32_t Kp = (uint32_t)KB * 128u;
     constexpr uint32_t kEl = E8 ? 1 : 4;
 
-    // waves 0, 1 bring A rows, waves 2, 3 B rows: 64 rows each, 8 rows a load
-    const bool isA = wave < 2;
-    const int64_t x0 = isA ? m0 : n0, rows = isA ? M : N, left = rows - x0;
-    const i32x4_t src =
-        buffer_rsrc((isA ? A : B) + x0 * Kp, (uint32_t)uniform((int)(left < kTile ? left : kTile)) * Kp);
-    uint32_t voff[8];                                // of load i, less its immediate offset
+    // a wave brings 32 rows of A and its share of B's, 8 rows a load
+    const i32x4_t srcA = buffer_rsrc(A + m0 * Kp, (uint32_t)uniform((int)min(M - m0, (int64_t)L::kM)) * Kp);
+    const i32x4_t srcB = buffer_rsrc(B + n0 * Kp, (uint32_t)uniform((int)min(N - n0, (int64_t)kTile)) * Kp);
+    uint32_t voff[4 + L::kLoadsB];                   // of load i, less its immediate offset
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        voff[i] = (uint32_t)(64 * (wave & 1) + 8 * i + (lane >> 3)) * Kp + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16) -
-                  (uint32_t)((i & 3) * 1024);
-    const uint32_t lds = lds_addr(sP) + (uint32_t)wave * 64u * kRowBytes, lds_s = lds_addr(sP) + kStage + wave * 256u;
-    // scales of 64 rows of the wave's operand, one row of the array a stage; of
-    // a tile, the one scale
-    const bool tile_scale = TILED && !isA;
+    for (int i = 0; i < 4 + L::kLoadsB; ++i)
+        voff[i] = (uint32_t)((i < 4 ? 32 : 8 * L::kLoadsB) * wave + 8 * (i & 3) + (lane >> 3)) * Kp +
+                  (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16) - (uint32_t)((i & 3) * 1024);
+    const uint32_t lds = lds_addr(sP) + (uint32_t)wave * 32u * kRowBytes;
+    const uint32_t lds_b = lds_addr(sP) + (uint32_t)(L::kM + 8 * L::kLoadsB * wave) * kRowBytes;
+    const uint32_t lds_s = lds_addr(sP) + kStage + wave * 256u;
+    // scales of 64 rows of one operand, one row of the array a stage; of a tile, the
+    // one scale (A's by the first WM waves, B's by two more, again, unused, by the rest)
+    const bool isA = wave < WM, tile_scale = TILED && !isA;
+    const int64_t rows = isA ? M : N, x0 = isA ? m0 : n0;
     const uint64_t sstep = uniform64((uint64_t)((tile_scale ? 1 : scale_pitch(rows)) * kEl));
     uint64_t sat = uniform64((uint64_t)(uintptr_t)(isA ? As : Bs) +       // of the stage that is loaded next
                              (uint64_t)(tile_scale ? (int64_t)tn * KB + kb0 : kb0 * scale_pitch(rows) + x0) * kEl);
-    const uint32_t srow = tile_scale ? 0u : (uint32_t)min((int64_t)(64 * (wave & 1) + lane), left - 1) * kEl;
-    // step i of stage kb's loads (rows 8i .. 8i + 7, at last the scales); m0 is
-    // written a step before the load that takes it
+    const uint32_t srow =
+        tile_scale ? 0u : (uint32_t)min((int64_t)(64 * (isA ? wave : wave & 1) + lane), rows - x0 - 1) * kEl;
+    // step i of stage kb's loads (8 rows each, at last the scales); m0 is written a
+    // step before the load that takes it
     auto load = [&](auto ic, int kb, int slot) {
         constexpr int i = decltype(ic)::value;
-        if constexpr (i < 8) dma_rows<(i & 3) * 1024>(src, voff[i], (uint32_t)kb * 128u);
+        if constexpr (i < kLoads - 1) dma_rows<(i & 3) * 1024>(i < 4 ? srcA : srcB, voff[i], (uint32_t)kb * 128u);
         else {
-            dma_scale<E8>(i32x4_t{(int)(uint32_t)sat, (int)(uint32_t)(sat >> 32), (int)(kTile * kEl), 0x00020000}, srow);
+            dma_scale<E8>(i32x4_t{(int)(uint32_t)sat, (int)(uint32_t)(sat >> 32), (int)(L::kM * kEl), 0x00020000}, srow);
             sat += kb + 1 < kb1 ? sstep : 0;
         }
-        if constexpr (i == 3) set_m0(lds + (uint32_t)(slot * kStageAll) + 4096u);
-        if constexpr (i == 7) set_m0(lds_s + (uint32_t)(slot * kStageAll));
+        if constexpr (i == 3) set_m0(lds_b + (uint32_t)(slot * kStageAll));
+        if constexpr (i == kLoads - 2) set_m0(lds_s + (uint32_t)(slot * kStageAll));
     };
     using F = Frag<E8, TILED>;
     // Half h of a lane's 32 bytes of row group i: chunks g and g + 4 of eight,
@@ -167,7 +175,7 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
         for (int s2 = 0; s2 < 2; ++s2) {
             const int at = s2 * 2 * kStageAll + ((g + 4 * h) ^ (l16 & 7)) * 16 + l16 * kRowBytes;
             base[s2][0][h] = sP + at + wm * 64 * kRowBytes;
-            base[s2][1][h] = sP + at + (kTile + wn * 64) * kRowBytes;
+            base[s2][1][h] = sP + at + (L::kM + wn * 64) * kRowBytes;
         }
     auto frag = [&](i32x8& f, int op, int i, int h, int slot) {
         const uint4 v = *reinterpret_cast<const uint4*>(base[slot / 2][op][h] + (slot % 2) * kStageAll + i * 16 * kRowBytes);
@@ -177,7 +185,7 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2) {
         scales[s2][0] = sP + s2 * 2 * kStageAll + kStage + wm * 256 + l16 * 4;
-        scales[s2][1] = sP + s2 * 2 * kStageAll + kStage + (2 + wn) * 256 + (TILED ? 0 : (E8 ? l16 : 4 * g) * 4);
+        scales[s2][1] = sP + s2 * 2 * kStageAll + kStage + (WM + wn) * 256 + (TILED ? 0 : (E8 ? l16 : 4 * g) * 4);
     }
     auto read_scales = [&](F& f, int slot) {
         const uint8_t* const a = scales[slot / 2][0] + (slot % 2) * kStageAll;
@@ -187,9 +195,17 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
             if (E8) f.ea[i] = *reinterpret_cast<const int*>(a + i * 64);
             else f.sa[i] = *reinterpret_cast<const float*>(a + i * 64);
             if (E8 && (!TILED || i == 0)) f.eb[i] = *reinterpret_cast<const int*>(b + i * 64);
-            if (!E8 && !TILED) f.sb[i] = *reinterpret_cast<const f32x4*>(b + i * 64);
         }
         if (TILED && !E8) f.st = *reinterpret_cast<const float*>(b);
+    };
+
+    // sb of four rows for each of a lane's row groups: held once, the next stage's
+    // read when the last product that takes them is added
+    f32x4 sb[TILED || E8 ? 1 : 4];
+    auto read_sb = [&](int j, int slot) {
+        if (!E8 && !TILED)
+            sb[TILED || E8 ? 0 : j] =
+                *reinterpret_cast<const f32x4*>(scales[slot / 2][1] + (slot % 2) * kStageAll + j * 64);
     };
 
     f32x4 acc[4][4];
@@ -202,7 +218,7 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
     // n and the loads of stage `kb` are issued.  A binary32 product is added three
     // products later, when it has left the matrix pipe (at least 14 instructions
     // after its own, whatever else stands between them).
-    auto turn = [&](F& f, F& n, int slot, int kb, int to) {
+    auto turn = [&](F& f, F& n, int slot, int kb, int to) __attribute__((always_inline)) {
         set_m0(lds + (uint32_t)(to * kStageAll));
         if (TILED && !E8) {
 #pragma unroll
@@ -213,7 +229,7 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
             constexpr int x = decltype(xc)::value, j = x / 4, i = x % 4;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                acc[j][i][e] = __builtin_fmaf(q[E8 ? 0 : x % 4][e], TILED ? f.sa[i] : f.sa[i] * f.sb[TILED || E8 ? 0 : j][e], acc[j][i][e]);
+                acc[j][i][e] = __builtin_fmaf(q[E8 ? 0 : x % 4][e], TILED ? f.sa[i] : f.sa[i] * sb[TILED || E8 ? 0 : j][e], acc[j][i][e]);
         };
         read_scales(n, slot);
         static_for<0, 16>([&](auto xc) {
@@ -223,13 +239,14 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
             else
                 product<AF>(q[x % 4], f.b[j], f.a[i]);
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (x < 9) load(xc, kb, to);
+            if constexpr (x < kLoads) load(xc, kb, to);
             frag(x < 8 ? n.a[x / 2 % 4] : n.b[x / 2 % 4], x / 8, x / 2 % 4, x % 2, slot);
             if constexpr (!E8 && x == 3) {           // no additions stand before this one
                 asm volatile("s_nop 5");
                 __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (!E8 && x >= 3) add(std::integral_constant<int, x - 3>{});
+            if constexpr (x >= 6 && x % 4 == 2) read_sb((x - 6) / 4, slot);
             __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (!E8) {
@@ -238,6 +255,7 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
             add(std::integral_constant<int, 13>{});
             add(std::integral_constant<int, 14>{});
             add(std::integral_constant<int, 15>{});
+            read_sb(3, slot);
         }
     };
 
@@ -258,32 +276,36 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
         F f, h;
         read_scales(f, 0);
 #pragma unroll
+        for (int j = 0; j < 4; ++j) read_sb(j, 0);
+#pragma unroll
         for (int i = 0; i < 8; ++i) {
             frag(f.a[i / 2], 0, i / 2, i % 2, 0);
             frag(f.b[i / 2], 1, i / 2, i % 2, 0);
         }
-        auto step = [&](F& cur, F& nxt, int k, int slot) {
+        auto step = [&](F& cur, F& nxt, int k, int slot) __attribute__((always_inline)) {
             // stage k + 1 has landed everywhere, every wave holds stage k
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads * (kRing - 2)) : "memory");
             turn(cur, nxt, (slot + 1) % kRing, min(kb0 + k + kRing, kb1 - 1), slot);
         };
+        constexpr int kTurns = kRing % 2 ? 2 * kRing : kRing;    // an even number: f and h change places
         int k = 0;
-        for (; k + 4 <= n; k += 4) {
-            step(f, h, k, 0);
-            step(h, f, k + 1, 1);
-            step(f, h, k + 2, 2);
-            step(h, f, k + 3, 3);
-        }
-        if (k < n) step(f, h, k, 0);
-        if (k + 1 < n) step(h, f, k + 1, 1);
-        if (k + 2 < n) step(f, h, k + 2, 2);
+        auto turns = [&](auto ic, int at) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            if constexpr (i % 2 == 0) step(f, h, at + i, i % kRing);
+            else step(h, f, at + i, i % kRing);
+        };
+        for (; k + kTurns <= n; k += kTurns)
+            static_for<0, kTurns>([&](auto ic) { turns(ic, k); });
+        static_for<0, kTurns - 1>([&](auto ic) {
+            if (k + decltype(ic)::value < n) turns(ic, k);
+        });
         // no load outlives the kernel's LDS, and the last products have landed
         asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     }
     if (parts > 1) {
         // this part's sums as [item][part][wave][j][i][lane][4]
-        float* out = part + ((int64_t)item * parts + p) * (kTile * kTile) + wave * 4096 + lane * 4;
+        float* out = part + ((int64_t)item * parts + p) * (L::kM * kTile) + wave * 4096 + lane * 4;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -312,7 +334,7 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
     const int64_t col = n0 + c * kPer;
     if (col >= N) return;
 #pragma unroll 4
-    for (int r = threadIdx.x / kPieces; r < kTile; r += 256 / kPieces) {
+    for (int r = threadIdx.x / kPieces; r < L::kM; r += L::kThreads / kPieces) {
         if (m0 + r >= M) break;
         const uint4 v = *reinterpret_cast<const uint4*>(sP + r * kPitch + c * 16);
         uint8_t* const d = (uint8_t*)C + ((m0 + r) * N + col) * kEs;
@@ -330,56 +352,72 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_kernel(int64_t M, int64_t N, 
     }
 }
 
-// The parts' sums of one sixteenth of a tile, in order.
-template <bool OUT_BF16>
+// The parts' sums of 1024 elements of a tile, in order.
+template <int WM, bool OUT_BF16>
 __global__ __launch_bounds__(256) void gemm_fp8_sum_kernel(int64_t M, int64_t N, int tiles_m, int tiles_n,
                                                            void* __restrict__ C, int parts,
                                                            const float* __restrict__ part) {
-    const int64_t item = blockIdx.x / 16;
+    using L = Tile<WM>;
+    constexpr int kPer = L::kM * kTile / 1024;
+    const int64_t item = blockIdx.x / kPer;
     int tm, tn;
-    tile_of((int)item, tiles_m, tiles_n, tm, tn);
-    const int at = (blockIdx.x % 16) * 256 + threadIdx.x, lane = at & 63, ji = at >> 6 & 15, wave = at >> 10;
-    const float* in = part + item * parts * (kTile * kTile) + at * 4;
+    tile_of((int)item, L::kGroup, tiles_m, tiles_n, tm, tn);
+    const int at = (blockIdx.x % kPer) * 256 + threadIdx.x, lane = at & 63, ji = at >> 6 & 15, wave = at >> 10;
+    const float* in = part + item * parts * (L::kM * kTile) + at * 4;
     f32x4 v = *reinterpret_cast<const f32x4*>(in);
-    for (int p = 1; p < parts; ++p) v += *reinterpret_cast<const f32x4*>(in + (int64_t)p * (kTile * kTile));
-    const int64_t m = (int64_t)tm * kTile + (wave >> 1) * 64 + (ji & 3) * 16 + (lane & 15);
+    for (int p = 1; p < parts; ++p) v += *reinterpret_cast<const f32x4*>(in + (int64_t)p * (L::kM * kTile));
+    const int64_t m = (int64_t)tm * L::kM + (wave >> 1) * 64 + (ji & 3) * 16 + (lane & 15);
     const int64_t n = (int64_t)tn * kTile + (wave & 1) * 64 + (ji >> 2) * 16 + (lane >> 4) * 4;
     if (m < M) store4<OUT_BF16>(C, m, n, N, v);
 }
 
 }  // namespace
 
-// Whether the 256 x 256 tiles take an E8M0 product faster: modelled times in
-// us, whole rounds of one tile a CU, each with a fixed part and one for each
-// block.  Model / measured (256 CUs): 8192 x 4096 x 21504 wide 555 / 534, small
-// 795 / 790; 2000 x 4096 x 4096 wide 63 / 56, small 41 / 38.
-static bool wide_is_faster(int64_t M, int64_t N, int64_t KB, int cus) {
-    auto rounds = [&](int64_t t) { return (double)(((M + t - 1) / t * ((N + t - 1) / t) + cus - 1) / cus); };
-    return KB > 0 && rounds(256) * (12.0 + 1.58 * KB) < rounds(128) * (2.0 + 0.58 * KB);
-}
-
-// Which kernel takes the product, and in how many parts along K the 128 x 128
-// tiles take it: as many as give every CU at most one part of at least eight
-// stages.  bytes: what the parts' partial sums take.
+// Which kernel takes a product, and in how many parts along K the tiles here take
+// it (never more than one workgroup a CU).  bytes: what the parts' sums take.
 struct Plan {
     enum { Skinny, Wide, Tiles } kernel = Tiles;
-    int cus = 0;
+    int cus = 0, wm = 2;
     int64_t tm = 0, tn = 0, parts = 1;
     size_t bytes = 0;
 };
 
+// The fastest by modelled times in us: rounds of one tile a CU, each with a fixed
+// part and one for each block, and for split tiles the sum's launch and the
+// partial sums' way out and back.  Model / measured on 256 CUs, M x N x K (F32: 128,
+// 256 rows; E8M0: 128, 256, wide):
+//   8192 x 21504 x 4096   F32 908 / 913, 706 / 707    E8M0 881 / 878, 649 / 655, 588 / 570
+//   2000 x 4096 x 4096    F32 43 / 43, 34 / 38        E8M0 42 / 36, 31 / 33, 53 / 56
+//   777 x 4096 x 21504    F32 98 / 96, 99 / 97        E8M0 94 / 84, 88 / 88, 257 / -
+//   1999 x 1360 x 3408    F32 19 / 18, 23 / 25        E8M0 18 / 16, 23 / 24, 46 / -
 static hipError_t make_plan(int64_t M, int64_t N, int64_t K, bool e8, Plan& p) {
-    hipError_t err = device_cus(&p.cus);
+    const hipError_t err = device_cus(&p.cus);
     if (err != hipSuccess) return err;
-    const int64_t KB = (K + 127) / 128;
-    p.tm = (M + kTile - 1) / kTile, p.tn = (N + kTile - 1) / kTile;
+    const int64_t KB = (K + 127) / 128, cus = p.cus;
     if (fp8_skinny(M, K)) {
         p.kernel = Plan::Skinny;
-    } else if (e8 && wide_is_faster(M, N, KB, p.cus)) {
+        return hipSuccess;
+    }
+    auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+    double best = 1e30;
+    for (int wm = 2; wm <= 4; wm += 2) {
+        const int64_t tm = up(M, 64 * wm), tn = up(N, kTile), tiles = tm * tn;
+        const double fixed = wm == 2 ? 3.7 : e8 ? 6.3 : 4.2;
+        const double each = wm == 2 ? (e8 ? 0.54 : 0.56) : e8 ? 0.77 : 0.92;
+        const int64_t most = std::max<int64_t>(std::min<int64_t>(cus / tiles, KB / 8), 1);
+        for (int64_t parts : {(int64_t)1, most}) {                    // whole, or split as far as it goes
+            const double bytes = parts > 1 ? (double)(tiles * parts) * (64 * wm) * kTile * 4 : 0.0;
+            const double us = (double)up(tiles * parts, cus) * (fixed + each * (double)up(KB, parts)) +
+                              (parts > 1 ? 4.0 + 2.0 * bytes / 5e6 : 0.0);
+            if (us < best) {
+                best = us;
+                p.wm = wm, p.tm = tm, p.tn = tn, p.parts = parts, p.bytes = (size_t)bytes;
+            }
+        }
+    }
+    if (e8 && KB > 0 && (double)up(up(M, 256) * up(N, 256), cus) * (5.5 + 1.5 * (double)KB) < best) {
         p.kernel = Plan::Wide;
-    } else {
-        p.parts = std::max<int64_t>(std::min<int64_t>(p.cus / std::max<int64_t>(p.tm * p.tn, 1), KB / 8), 1);
-        if (p.parts > 1) p.bytes = (size_t)(p.tm * p.tn * p.parts) * kTile * kTile * 4;
+        p.parts = 1, p.bytes = 0;
     }
     return hipSuccess;
 }
@@ -393,15 +431,15 @@ static hipError_t run_plan(const Plan& p, int64_t M, int64_t N, int64_t K, const
     if (p.kernel == Plan::Wide)
         return launch_gemm_fp8_wide(M, N, K, p.cus, a, as, a_fmt, b, bs, tiled, c, c_bf16, s);
     const int64_t KB = (K + 127) / 128, tm = p.tm, tn = p.tn, parts = p.parts;
-    auto go = [&](auto af, auto e, auto tl, auto bf) {
-        hipLaunchKernelGGL((gemm_fp8_kernel<decltype(af)::value, decltype(e)::value, decltype(tl)::value, decltype(bf)::value>),
-                           dim3((unsigned)(tm * tn * parts)), dim3(256), 0, s, M, N, (int)KB, (int)tm, (int)tn, a, as, b,
-                           bs, c,
-                           (int)parts, part);
+    auto go = [&](auto wm, auto af, auto e, auto tl, auto bf) {
+        constexpr int kWM = decltype(wm)::value;
+        hipLaunchKernelGGL((gemm_fp8_kernel<kWM, decltype(af)::value, decltype(e)::value, decltype(tl)::value, decltype(bf)::value>),
+                           dim3((unsigned)(tm * tn * parts)), dim3(128 * kWM), 0, s, M, N, (int)KB, (int)tm, (int)tn, a,
+                           as, b, bs, c, (int)parts, part);
         hipError_t e2 = hipGetLastError();
         if (e2 != hipSuccess || parts == 1) return e2;
-        hipLaunchKernelGGL((gemm_fp8_sum_kernel<decltype(bf)::value>), dim3((unsigned)(tm * tn * 16)), dim3(256), 0, s,
-                           M, N, (int)tm, (int)tn, c, (int)parts, part);
+        hipLaunchKernelGGL((gemm_fp8_sum_kernel<kWM, decltype(bf)::value>), dim3((unsigned)(tm * tn * 8 * kWM)), dim3(256),
+                           0, s, M, N, (int)tm, (int)tn, c, (int)parts, part);
         return hipGetLastError();
     };
     using Y = std::true_type;
@@ -409,7 +447,12 @@ static hipError_t run_plan(const Plan& p, int64_t M, int64_t N, int64_t K, const
     auto with = [](bool v, auto&& f) { return v ? f(Y{}) : f(F{}); };
     return with(a_fmt == Fp8::E5M2, [&](auto af) {
         return with(e8, [&](auto e) {
-            return with(tiled, [&](auto tl) { return with(c_bf16, [&](auto bf) { return go(af, e, tl, bf); }); });
+            return with(tiled, [&](auto tl) {
+                return with(c_bf16, [&](auto bf) {
+                    if (p.wm == 4) return go(std::integral_constant<int, 4>{}, af, e, tl, bf);
+                    return go(std::integral_constant<int, 2>{}, af, e, tl, bf);
+                });
+            });
         });
     });
 }
