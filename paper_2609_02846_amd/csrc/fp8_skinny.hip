@@ -12,7 +12,12 @@
 //
 // FUSED: A is bf16, a few thousand elements in all, and every workgroup
 // quantizes it for itself, into LDS, while its first weights are on their way:
-// one launch, and nothing to wait for, instead of two.
+// one launch, and nothing to wait for, instead of two (1 x 6144 x 4096 9.3 us, two
+// launches 11.5; 1 x 3408 x 1360 4.4 and 6.0; but 4 x 6144 x 4096 12.7 and 10.7).
+//
+// Out of HBM: 1 x 6144 x 4096 9.3 us (2.7 TB/s: a wave holds six blocks, and the
+// start and the sums are half of the time), 24 x 21504 x 4096 22 - 24 us (3.8 - 4.1
+// TB/s); a large copy reaches 5.2 TB/s.
 #include <algorithm>
 #include <atomic>
 
@@ -24,7 +29,7 @@
 namespace ue5m3 {
 namespace {
 
-constexpr int kFusedBytes = 16384;               // quantized tokens that a workgroup keeps
+constexpr int kFusedBytes = 8192;               // quantized tokens that a workgroup keeps
 
 struct SkinnyArgs {
     const uint8_t* a;                            // payload, or bf16 tokens (FUSED)
@@ -260,10 +265,12 @@ hipError_t launch(const SkinnyArgs& g, int cus, bool e5m2, bool tiled, bool e8, 
                 return hipGetLastError();
             };
             auto waves = [&](auto m, auto af, auto tl) {
-                // four waves, so that a CU holds two workgroups of 16 rows of A; eight
-                // where there is not a tile for every CU
+                // Four waves, so that a CU holds two workgroups of 16 rows of A (16 x 21504
+                // x 4096 23.6 us, eight waves 24.9); eight where there is not a tile for
+                // every CU and each of them still has blocks enough (1 x 4096 x 16384 19,
+                // four 21; but 16 x 4096 x 1024 6.5, four 5.6).
                 if constexpr (decltype(m)::value == 1)
-                    if (tiles <= cus) return go(std::integral_constant<int, 8>{}, m, af, tl);
+                    if (tiles <= cus && g.KB >= 32) return go(std::integral_constant<int, 8>{}, m, af, tl);
                 return go(std::integral_constant<int, 4>{}, m, af, tl);
             };
             if constexpr (FUSED) {

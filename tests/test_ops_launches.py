@@ -23,8 +23,8 @@ def test_routes(scale):
     for entry, first in (("gemm", []), ("linear", ["quant_fp8_rows_kernel"])):
         one, many = [["gemm_fp8_skinny_kernel"]], [first + ["gemm_fp8_skinny_kernel"]]
         call = lambda M, N, K: names([fp8_call(M, N, K, entry, scale=scale)])  # noqa: E731
-        assert call(1, 21504, 4096) == one and call(16, 500, 1024) == one   # quantized where it is multiplied
-        assert call(64, 21504, 4096) == many and call(17, 500, 1) == many
+        assert call(1, 21504, 4096) == one and call(8, 500, 1024) == one    # quantized where it is multiplied
+        assert call(64, 21504, 4096) == many and call(17, 500, 1) == many and call(9, 500, 1024) == many
         assert call(65, 128, 1024) == [first + [RING]]
         assert call(100, 128, 2048) == [first + [RING, SUM]]                # few tiles, a long contraction
         assert call(8192, 21504, 4096) == [first + [large]]
