@@ -22,6 +22,7 @@ Language Model Pretraining" (arXiv 2609.02846):
 * ``rht``      -- the 16-point randomized Hadamard transform of the wgrad
   operands (the "UE5M3 with Transformer Engine settings" recipe) and the
   quantizer on transformed values.
+* ``fp8``      -- the 8-bit block quantizers (one scale for each 128).
 * ``accumulate`` -- the probe-matched output model (eq:issue-partial,
   eq:issue-rz, eq:final-grid, eq:grid-denominator): 64-product RNE
   partials, toward-zero cross-group adds, optional 1/d product-lattice snap.

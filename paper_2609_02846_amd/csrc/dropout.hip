@@ -13,7 +13,8 @@
 //
 // Bound: HBM (read, optional residual, write), with the generator close
 // behind: ten rounds cost about 20 multiplies of 64 bits and 20 XORs for eight
-// elements; 32 bits for each element would double that.
+// elements; 32 bits for each element would double that.  8192 x 4096 bf16 with a
+// residual 38 us (5.3 TB/s), without 23.6 (5.7): what a large copy reaches.
 #include <cmath>
 
 #include "codec.hpp"

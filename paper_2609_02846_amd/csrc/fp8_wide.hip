@@ -13,6 +13,9 @@
 // the 128 x 128 tiles need for as many products, which were held up there by
 // the loads (half of each wave's time it waited to issue one).  LDS reads and
 // loads stand between the products, one of each, so that neither comes in bursts.
+// 8192 x 21504 x 4096 530 - 615 us (2350 - 2720 TFLOP/s), 8192 x 4096 x 21504 525, 8192^3
+// 397 (2770; without the lines fetched ahead into L2 12% slower), where the
+// library's product under one scale for each tensor takes 393.
 #include "fp8.hpp"
 #include "fp8_tile.hpp"
 #include "gemm_regs.hpp"
