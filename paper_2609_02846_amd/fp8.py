@@ -58,8 +58,8 @@ def forward_product(x, w, scale, need_dx, need_dw):
     _bf16_2d(w, "weight")
     T, K = x.shape
     N = w.shape[0]
-    if w.shape[1] != K:
-        raise ValueError(f"weight has {w.shape[1]} columns, the input {K}")
+    if w.shape[1] != K or w.device != x.device:
+        raise ValueError(f"weight has {w.shape[1]} columns on {w.device}, the input {K} on {x.device}")
     kind, size = _SCALE[scale]
     lib, stream = load_library(), _stream()
     saved, temp = _forward_layout(T, K, N, size, need_dx, need_dw)

@@ -283,6 +283,31 @@ def test_few_rows_by_many_columns(M, N, K, tiled, scale):
         product_check(ue.linear_fp8(x, b, sb, out_dtype=torch.float32), A, B, K, f"serve {M} {N} {K}")
 
 
+# more rounds of 128 rows than of 256; too few tiles of 256 rows for every CU, so split
+TALL = [(1990, 2501, 300), (630, 3301, 12700)]
+
+
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("a_fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("tiled", [False, True])
+def test_tall_tiles(scale, a_fmt, tiled):
+    """Products of 256 x 128 tiles: every row at some columns and every column at some rows."""
+    for M, N, K in TALL:
+        say("tall", M, N, K, scale, a_fmt, tiled)
+        a, sa, b, sb, A, B = operands(M, N, K, scale, a_fmt, tiled, M)
+        blk = dict(b_blk="tile" if tiled else "row")
+        guard = torch.full((M * N + 64,), 7.0, device="cuda")
+        c = ue.gemm_fp8("nt", M, N, K, a, sa, b, sb, out=guard[:M * N].view(M, N), **blk)
+        assert (guard[M * N:] == 7.0).all()
+        half = ue.gemm_fp8("nt", M, N, K, a, sa, b, sb, **blk)
+        m = torch.tensor([0, 15, 63, 64, 127, 255, 256, 300, M - 1], device="cuda")
+        n = torch.tensor([0, 3, 15, 64, 127, 128, 200, N - 2, N - 1], device="cuda")
+        for rows, cols in ((torch.arange(M, device="cuda"), n), (m, torch.arange(N, device="cuda"))):
+            As, Bs = (A[0][rows], A[1][rows], A[2]), (B[0][cols], B[1][cols], B[2])
+            product_check(c[rows][:, cols], As, Bs, K, f"{M} {N} {K} fp32")
+            product_check(half[rows][:, cols], As, Bs, K, f"{M} {N} {K} bf16", True)
+
+
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 def test_bad_values_stay_in_their_row(scale):
     """A NaN token spoils its own outputs and nothing else."""

@@ -3,6 +3,7 @@ and their workspaces, on the host alone (256 compute units)."""
 
 import pytest
 
+import test_gpu_fp8 as fp8_tests
 from host_launches import fp8_call, launches, norm_grad_call, together
 
 
@@ -29,6 +30,16 @@ def test_routes(scale):
         assert call(100, 128, 2048) == [first + [RING, SUM]]                # few tiles, a long contraction
         assert call(8192, 21504, 4096) == [first + [large]]
     assert names([fp8_call(300, 300, 0, "linear", scale=scale)]) == [[RING]]
+
+
+def test_tall_tiles_run_at_the_sizes_their_test_has():
+    """The choice rests on modelled times: the test of the 256 x 128 tiles has to
+    be at sizes that run on them, whole and split."""
+    for M, N, K in fp8_tests.TALL:
+        for scale, tiled in (("f32", False), ("f32", True), ("e8m0", False), ("e8m0", True)):
+            (status, kernels), = launches([fp8_call(M, N, K, scale=scale, tiled=tiled)])
+            assert status == 0 and kernels[0][2] == 512, (M, N, K, scale, kernels)      # eight waves
+            assert ("sum" in kernels[-1][0]) == (K > 4096), (M, N, K, scale, kernels)
 
 
 @pytest.mark.parametrize("call", [fp8_call(100, 128, 2048, capturing=True),
