@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
 
     enter(0);
     enter_ahead();
-    fb = min(2 + kAhead, KB - 1);
+    fb = min(1 + kAhead, KB - 1);
     start(0);
     asm volatile("s_nop 0");
     static_for<0, 18>([&](auto ic) {
@@ -219,6 +219,11 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
         load(ic, 1);
         asm volatile("s_nop 0");
     });
+    // (as in every turn: the first one's wait leaves one load out, and the last code
+    // of stage 1 must not be that one)
+    set_m0(lds_d);
+    asm volatile("s_nop 0");
+    ahead();
 
     int b = 0;
     for (int k = 0; k < nw; ++k) {
