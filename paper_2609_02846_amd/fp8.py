@@ -64,7 +64,7 @@ def forward_product(x, w, scale, need_dx, need_dw):
     lib, stream = load_library(), _stream()
     saved, temp = _forward_layout(T, K, N, size, need_dx, need_dw)
     work, y = _buffer(temp, x), torch.empty((T, N), dtype=torch.bfloat16, device=x.device)
-    keep = _buffer(saved, x) if saved.bytes else None
+    keep = _buffer(saved, x) if need_dx or need_dw else None
     t, k = work.data_ptr(), keep.data_ptr() if keep is not None else 0
     xt, sxt = (k + saved.xt, k + saved.sxt) if need_dw else (None, None)
     wt, swt = (k + saved.wt, k + saved.swt) if need_dx else (None, None)

@@ -393,6 +393,13 @@ def test_module_empty_and_frozen():
     assert y.shape == (0, 130) and g[0].shape == (0, 200) and not g[1].any()
 
 
+def test_no_tokens_with_a_weight_gradient_alone():
+    w = tensor(130, 200, 2).requires_grad_()
+    y = fp8_linear(torch.empty(0, 200, device="cuda", dtype=torch.bfloat16), w)
+    dw, = torch.autograd.grad(y, w, torch.empty_like(y))
+    assert y.shape == (0, 130) and dw.shape == w.shape and not dw.any()
+
+
 def test_streams_and_graph():
     """A serving call on another stream, and captured: every replay equals the
     eager result, with eager work between the replays."""
