@@ -34,22 +34,35 @@ def dropout(x, p, seed, tensor_id=0, residual=None):
 
 
 class Dropout(torch.nn.Module):
-    """Dropout with its own key: call c of the module in training draws with
-    key ``seed`` + c and tensor id ``layer_id``; in evaluation x (plus the
-    residual) passes."""
+    """Dropout with a key of its own for each call in training and tensor id
+    ``layer_id``; in evaluation x (plus the residual) passes.
 
-    def __init__(self, p=0.1, seed=0, layer_id=0):
+    Without ``seed`` a call's key comes from torch's CPU generator, so that
+    ``torch.manual_seed`` and the generator's state bring a run's masks back,
+    and a call that activation checkpointing repeats, with that state
+    restored, draws the mask of the first.  With ``seed`` call c draws with key
+    ``seed`` + c: modules of one seed need different ``layer_id``s, or all of
+    them drop the same elements, and the seeds of ranks have to be further
+    apart than a run has calls."""
+
+    def __init__(self, p=0.1, seed=None, layer_id=0):
         super().__init__()
         if not 0.0 <= p <= 1.0:
             raise ValueError("p must be in [0, 1]")
-        self.p, self.seed, self.layer_id, self.calls = float(p), int(seed), int(layer_id), 0
+        self.p, self.seed, self.layer_id, self.calls = float(p), None if seed is None else int(seed), int(layer_id), 0
+
+    def next_key(self):
+        """The key of one call."""
+        if self.seed is None:
+            return torch.randint(-2 ** 63, 2 ** 63 - 1, (), device="cpu").item() & (2 ** 64 - 1)
+        key = (self.seed + self.calls) & (2 ** 64 - 1)
+        self.calls += 1
+        return key
 
     def forward(self, x, residual=None):
         if not self.training:
             return x if residual is None else residual + x
-        key = (self.seed + self.calls) & (2 ** 64 - 1)
-        self.calls += 1
-        return dropout(x, self.p, key, self.layer_id, residual)
+        return dropout(x, self.p, self.next_key(), self.layer_id, residual)
 
     def extra_repr(self):
         return f"p={self.p}"

@@ -78,9 +78,10 @@ def sublayer(x, gain, bias, weight, p=0.1, seed=0, tensor_id=0, eps=1e-5, scale=
 
 class PreNormSublayer(torch.nn.Module):
     """The branch with its parameters.  In evaluation dropout passes and, after
-    ``linear.freeze()``, the product takes the quantized weight."""
+    ``linear.freeze()``, the product takes the quantized weight.  ``seed`` and
+    ``layer_id`` are dropout's (see ``Dropout``)."""
 
-    def __init__(self, features, p=0.1, eps=1e-5, scale="e8m0", grad_fmt="e4m3", seed=0, layer_id=0, device="cuda"):
+    def __init__(self, features, p=0.1, eps=1e-5, scale="e8m0", grad_fmt="e4m3", seed=None, layer_id=0, device="cuda"):
         super().__init__()
         self.norm = LayerNorm(features, eps, device=device)
         self.linear = Fp8Linear(features, features, scale, grad_fmt, device)
@@ -90,7 +91,5 @@ class PreNormSublayer(torch.nn.Module):
         if not self.training or self.linear.frozen is not None:
             return self.dropout(self.linear(self.norm(x)), residual=x)
         d = self.dropout
-        key = (d.seed + d.calls) & (2 ** 64 - 1)
-        d.calls += 1
-        return sublayer(x, self.norm.weight, self.norm.bias, self.linear.weight, d.p, key, d.layer_id, self.norm.eps,
-                        self.linear.scale, self.linear.grad_fmt)
+        return sublayer(x, self.norm.weight, self.norm.bias, self.linear.weight, d.p, d.next_key(), d.layer_id,
+                        self.norm.eps, self.linear.scale, self.linear.grad_fmt)
