@@ -43,7 +43,9 @@ class Dropout(torch.nn.Module):
     restored, draws the mask of the first.  With ``seed`` call c draws with key
     ``seed`` + c: modules of one seed need different ``layer_id``s, or all of
     them drop the same elements, and the seeds of ranks have to be further
-    apart than a run has calls."""
+    apart than a run has calls.  A call inside a backward pass, where
+    checkpointing repeats one, is refused then: which call it repeats the
+    count does not tell."""
 
     def __init__(self, p=0.1, seed=None, layer_id=0):
         super().__init__()
@@ -55,6 +57,9 @@ class Dropout(torch.nn.Module):
         """The key of one call."""
         if self.seed is None:
             return torch.randint(-2 ** 63, 2 ** 63 - 1, (), device="cpu").item() & (2 ** 64 - 1)
+        if torch._C._current_graph_task_id() != -1:
+            raise RuntimeError("a module with a seed of its own counts its calls, and a call repeated in the backward "
+                               "pass would draw another mask: leave seed out to checkpoint it")
         key = (self.seed + self.calls) & (2 ** 64 - 1)
         self.calls += 1
         return key

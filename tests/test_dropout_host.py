@@ -39,6 +39,16 @@ def test_gradients_under_checkpointing(reentrant):
         assert torch.equal(got, exp)
 
 
+@pytest.mark.parametrize("reentrant", [True, False])
+def test_a_counted_key_is_refused_in_a_recomputed_call(reentrant):
+    """With a seed of its own the module counts its calls and cannot tell which
+    one is repeated: an error, not another mask's gradients."""
+    x, w = torch.randn(30, 40), torch.randn(40)
+    gradients(Dropout(0.3, seed=5), x, w)
+    with pytest.raises(RuntimeError, match="seed"):
+        gradients(Dropout(0.3, seed=5), x, w, reentrant)
+
+
 def test_modules_and_runs():
     """By default modules draw unrelated masks, and torch's generator state
     brings a run's masks back."""

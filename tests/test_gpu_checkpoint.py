@@ -46,3 +46,10 @@ def test_a_stack_has_a_mask_for_each_layer():
     x = torch.ones(64, 256, device="cuda", dtype=torch.bfloat16)
     a, b = Dropout(0.5), Dropout(0.5)
     assert not torch.equal(a(x), b(x)) and not torch.equal(a(x), a(x))
+
+
+@pytest.mark.parametrize("reentrant", [True, False])
+def test_counted_keys_are_refused(reentrant):
+    x = torch.randn(8, 128, device="cuda").to(torch.bfloat16)
+    with pytest.raises(RuntimeError, match="seed"):
+        outcome([PreNormSublayer(128, seed=4)], x, reentrant)
