@@ -69,5 +69,20 @@ class Dropout(torch.nn.Module):
             return x if residual is None else residual + x
         return dropout(x, self.p, self.next_key(), self.layer_id, residual)
 
+    # The count goes with the parameters, so that a resumed run does not draw its
+    # first masks again.
+    def _save_to_state_dict(self, destination, prefix, keep_vars):
+        super()._save_to_state_dict(destination, prefix, keep_vars)
+        if self.seed is not None:
+            destination[prefix + "calls"] = torch.tensor(self.calls, device="cpu")
+
+    def _load_from_state_dict(self, state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, errors):
+        super()._load_from_state_dict(state_dict, prefix, local_metadata, strict, missing_keys, unexpected_keys, errors)
+        key = prefix + "calls"
+        if key in state_dict:
+            self.calls = int(state_dict[key])
+            if key in unexpected_keys:
+                unexpected_keys.remove(key)
+
     def extra_repr(self):
         return f"p={self.p}"

@@ -71,3 +71,22 @@ def test_seeded_calls():
     calls = [m(x), m.eval()(x), m.train()(x)]
     assert torch.equal(calls[0], module.dropout_forward(x, 0.5, 9, 2)) and calls[1] is x
     assert torch.equal(calls[2], module.dropout_forward(x, 0.5, 10, 2))
+
+
+def test_a_resumed_run_goes_on_with_the_count():
+    """The count of a seeded module is part of the state dict; a state without
+    one, or with one that the module has no use for, loads too."""
+    x = torch.ones(100)
+    m = torch.nn.Sequential(Dropout(0.5, seed=9), torch.nn.Identity())
+    m(x), m(x)
+    state = m.state_dict()
+    want = m(x)
+    resumed = torch.nn.Sequential(Dropout(0.5, seed=9), torch.nn.Identity())
+    resumed.load_state_dict(state)
+    assert torch.equal(resumed(x), want)
+    assert all(isinstance(v, torch.Tensor) for v in state.values())
+    m.load_state_dict({})                             # from before there was a count
+    torch.nn.Sequential(Dropout(0.5), torch.nn.Identity()).load_state_dict(state)
+    assert not torch.nn.Sequential(Dropout(0.5)).state_dict()
+    with pytest.raises(RuntimeError, match="other"):
+        m.load_state_dict({"0.other": torch.ones(1)})
