@@ -147,10 +147,24 @@ def fp8_linear(x, weight, scale="e8m0", grad_fmt="e4m3"):
     return y if x.dim() == 2 else y.reshape(*x.shape[:-1], weight.shape[0])
 
 
+class _FrozenFn(torch.autograd.Function):
+    """The serving call where gradients are recorded: in a sum with another
+    branch they would reach that one alone, without a word."""
+
+    @staticmethod
+    def forward(ctx, x, w, scales):
+        return linear_fp8(x.contiguous(), w, scales)
+
+    @staticmethod
+    def backward(ctx, dy):
+        raise RuntimeError("a frozen Fp8Linear has no gradients: unfreeze() it, or call it under torch.no_grad()")
+
+
 class Fp8Linear(torch.nn.Module):
     """Linear layer without bias in 8-bit floating point (see ``fp8_linear``).
     ``freeze()`` quantizes the weight once for serving: forward calls then take
-    the quantized weight and give no gradients, until ``unfreeze()``."""
+    the quantized weight, and a backward pass through one raises, until
+    ``unfreeze()``."""
 
     def __init__(self, in_features, out_features, scale="e8m0", grad_fmt="e4m3", device="cuda"):
         super().__init__()
@@ -171,8 +185,9 @@ class Fp8Linear(torch.nn.Module):
     def forward(self, x):
         if self.frozen is None:
             return fp8_linear(x, self.weight, self.scale, self.grad_fmt)
-        with torch.no_grad():
-            return linear_fp8(x.contiguous(), *self.frozen)
+        if torch.is_grad_enabled() and x.requires_grad:
+            return _FrozenFn.apply(x, *self.frozen)
+        return linear_fp8(x.contiguous(), *self.frozen)
 
     def extra_repr(self):
         return f"in_features={self.in_features}, out_features={self.out_features}, scale={self.scale}"
