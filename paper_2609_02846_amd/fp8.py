@@ -164,7 +164,8 @@ class Fp8Linear(torch.nn.Module):
     """Linear layer without bias in 8-bit floating point (see ``fp8_linear``).
     ``freeze()`` quantizes the weight once for serving: forward calls then take
     the quantized weight, and a backward pass through one raises, until
-    ``unfreeze()``."""
+    ``unfreeze()``.  A weight changed in place while frozen (an optimizer's
+    step) needs another ``freeze()``."""
 
     def __init__(self, in_features, out_features, scale="e8m0", grad_fmt="e4m3", device="cuda"):
         super().__init__()
@@ -180,6 +181,19 @@ class Fp8Linear(torch.nn.Module):
 
     def unfreeze(self):
         self.frozen = None
+        return self
+
+    # What was quantized goes with the weight: a loaded one is quantized in its
+    # place, a moved one takes it along.
+    def _load_from_state_dict(self, *args):
+        super()._load_from_state_dict(*args)
+        if self.frozen is not None:
+            self.freeze()
+
+    def _apply(self, fn, recurse=True):
+        super()._apply(fn, recurse)
+        if self.frozen is not None:
+            self.frozen = tuple(t.to(self.weight.device) for t in self.frozen)
         return self
 
     def forward(self, x):

@@ -45,3 +45,22 @@ def test_a_frozen_branch_gives_no_partial_gradients(training):
         y.sum().backward()
     with torch.no_grad():
         assert not m(x).requires_grad
+
+
+def test_a_loaded_weight_is_quantized_again():
+    """A frozen layer answers with the weight that it holds, not with the one
+    that it was frozen with."""
+    x = torch.randn(3, 16).to(torch.bfloat16)
+    layer, other = Fp8Linear(16, 8, device="cpu").freeze(), Fp8Linear(16, 8, device="cpu")
+    stack = torch.nn.Sequential(layer)
+    with torch.no_grad():
+        stack.load_state_dict({"0.weight": other.weight.clone()})
+        assert torch.equal(stack(x), other.freeze()(x))
+    assert layer.frozen is not None
+
+
+def test_a_moved_layer_stays_whole():
+    """.to() takes the quantized weight along."""
+    layer = Fp8Linear(16, 8, device="cpu").freeze()
+    layer.to("meta")
+    assert all(t.device.type == "meta" for t in (layer.weight, *layer.frozen))
