@@ -5,7 +5,7 @@ backward pass computes it again, so nothing but the key is kept."""
 import torch
 from torch.autograd.function import once_differentiable
 
-from .operators import dropout_forward
+from .operators import dropout_forward, recorded
 
 
 class _DropoutFn(torch.autograd.Function):
@@ -28,7 +28,7 @@ def dropout(x, p, seed, tensor_id=0, residual=None):
     reciprocal of what is kept."""
     x = x.contiguous()
     residual = None if residual is None else residual.contiguous()
-    if torch.is_grad_enabled() and (x.requires_grad or (residual is not None and residual.requires_grad)):
+    if recorded(x, residual):
         return _DropoutFn.apply(x, residual, float(p), int(seed), int(tensor_id))
     return dropout_forward(x, p, seed, tensor_id, residual)
 

@@ -15,7 +15,7 @@ from torch.autograd.function import once_differentiable
 
 from . import NN, NT, OUT_BF16, TN, _bf16_2d, _check, _numel, _stream, load_library
 from .linear import _Layout
-from .operators import COL128T, ROW128, TILE128, linear_fp8, pad128, quantize_fp8_tiles, scale_pitch
+from .operators import COL128T, ROW128, TILE128, linear_fp8, pad128, quantize_fp8_tiles, recorded, scale_pitch
 
 _GRAD = {"e4m3": 0, "e5m2": 1}
 _SCALE = {"f32": (0, 4), "e8m0": (1, 1)}             # code, bytes of a scale
@@ -138,9 +138,8 @@ def fp8_linear(x, weight, scale="e8m0", grad_fmt="e4m3"):
     gradient, "e4m3" or "e5m2"."""
     _check_formats(scale, grad_fmt)
     x2 = _flat(x, weight.shape[1])
-    grad = torch.is_grad_enabled()
-    need_dx, need_dw = grad and x.requires_grad, grad and weight.requires_grad
-    if need_dx or need_dw:
+    if recorded(x2, weight):
+        need_dx, need_dw = x.requires_grad, weight.requires_grad
         y = _Fp8LinearFn.apply(x2, weight, scale, grad_fmt, need_dx, need_dw)
     else:
         y, _ = forward_product(x2, weight, scale, False, False)
@@ -199,7 +198,7 @@ class Fp8Linear(torch.nn.Module):
     def forward(self, x):
         if self.frozen is None:
             return fp8_linear(x, self.weight, self.scale, self.grad_fmt)
-        if torch.is_grad_enabled() and x.requires_grad:
+        if recorded(x):
             return _FrozenFn.apply(x, *self.frozen)
         return linear_fp8(x.contiguous(), *self.frozen)
 

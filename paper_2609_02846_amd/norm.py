@@ -4,7 +4,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import _check, _stream, load_library
-from .operators import _TYPES, _like, layer_norm_forward, norm_args
+from .operators import _TYPES, _like, layer_norm_forward, norm_args, recorded
 
 # Small calls are bound by the host: the autograd function marshals the library
 # calls itself, and both statistics of a row lie in one buffer.
@@ -47,8 +47,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     gradients.  ``weight`` and ``bias`` have x's type or fp32; their gradients
     are summed in fp32 in a fixed order."""
     x = x.contiguous()
-    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or
-                                    (bias is not None and bias.requires_grad)):
+    if recorded(x, weight, bias):
         return _LayerNormFn.apply(x, weight, bias, float(eps))
     return layer_norm_forward(x, weight, bias, eps)
 

@@ -19,6 +19,7 @@ with pad() up to a multiple of 128 and pitch() up to one of 16.
 import contextlib
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _LAYOUTS, NT, OUT_BF16, OUT_F32, TN, _check, _dev_buf, _numel, _ptr, _stream, load_library
 
@@ -67,6 +68,16 @@ def _like(t, x, name):
     if t is not None and _tensor(t, name, (x.dtype,), x).shape != x.shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(x.shape)} needed")
     return t
+
+
+def recorded(*tensors):
+    """Whether autograd records a call on these tensors (or None).  Tangents of
+    forward-mode differentiation are refused: no operator here has any, and
+    where nothing is recorded they would be dropped."""
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None
+                                              for t in tensors):
+        raise NotImplementedError("the operators have no forward-mode derivatives")
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 # ------------------------------------------------------------- layer norm --

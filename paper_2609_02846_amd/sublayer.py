@@ -14,7 +14,7 @@ from . import _check, _stream, load_library
 from .dropout import Dropout
 from .fp8 import Fp8Linear, _check_formats, _flat, backward_products, forward_product
 from .norm import LayerNorm
-from .operators import BF16, dropout_forward, layer_norm_forward, norm_args
+from .operators import BF16, dropout_forward, layer_norm_forward, norm_args, recorded
 
 
 class _SublayerFn(torch.autograd.Function):
@@ -66,7 +66,7 @@ def sublayer(x, gain, bias, weight, p=0.1, seed=0, tensor_id=0, eps=1e-5, scale=
     if tuple(weight.shape) != (C, C):
         raise ValueError(f"the branch's weight must be [{C}, {C}] to add to its input")
     x2 = _flat(x, C)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, gain, bias, weight)):
+    if recorded(x2, gain, bias, weight):
         y = _SublayerFn.apply(x2, gain, bias, weight, float(p), int(seed) & (2 ** 64 - 1), int(tensor_id) & 0xFFFFFFFF,
                               float(eps), scale, grad_fmt, weight.requires_grad)
     else:
