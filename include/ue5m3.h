@@ -21,7 +21,8 @@
  *   ue5m3_layer_norm_grad, the split-tile partials of ue5m3_gemm_fp8, and the
  *   quantized tokens and split-tile partials of ue5m3_linear_fp8.  A workspace
  *   is allocated (hipMalloc) by the first call on that pair that needs it,
- *   or needs a larger one; a replaced workspace is never freed before the
+ *   or needs a larger one (twice the old one's size at least, where there
+ *   is room for it); a replaced workspace is never freed before the
  *   process ends, so work already enqueued or captured in a graph keeps a
  *   valid buffer.  Calls on one stream use a workspace in stream order;
  *   streams are told apart by handle value, so a stream should be destroyed

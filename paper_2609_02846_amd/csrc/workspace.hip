@@ -3,6 +3,9 @@
 // A workspace that has to grow is replaced by a larger allocation and the
 // old one is kept, never freed, until the process ends: launches already
 // enqueued on the stream, or recorded in a captured graph, may still use it.
+// The new one is at least twice as large as the old one where that much
+// memory is left: over calls that grow without end, as the token counts of a
+// server's prompts do, all of them together take less than twice the last.
 // Nothing here synchronizes.  A stream that is being captured cannot
 // allocate (hipMalloc is not a capturable operation), so a call that would
 // need a new or larger workspace during capture fails instead.
@@ -57,7 +60,14 @@ hipError_t grow(WorkspaceSlot& x, hipStream_t s, size_t bytes) {
     if (e != hipSuccess) return e;
     if (cs != hipStreamCaptureStatusNone) return hipErrorStreamCaptureUnsupported;
     void* p = nullptr;
-    if ((e = hipMalloc(&p, bytes)) != hipSuccess) return e;
+    const size_t need = bytes;
+    if (bytes < 2 * x.bytes) bytes = 2 * x.bytes;
+    e = hipMalloc(&p, bytes);
+    if (e != hipSuccess && bytes > need) {
+        (void)hipGetLastError();                 // handled here: not the next launch's
+        e = hipMalloc(&p, bytes = need);
+    }
+    if (e != hipSuccess) return e;
     x.ptr = p;                                   // a replaced buffer stays allocated
     x.bytes = bytes;
     return hipSuccess;
