@@ -60,13 +60,15 @@ hipError_t grow(WorkspaceSlot& x, hipStream_t s, size_t bytes) {
     if (e != hipSuccess) return e;
     if (cs != hipStreamCaptureStatusNone) return hipErrorStreamCaptureUnsupported;
     void* p = nullptr;
+    auto allocate = [&](size_t n) {
+        const hipError_t r = hipMalloc(&p, n);
+        if (r != hipSuccess) (void)hipGetLastError();   // this call's status, not the next launch's
+        return r;
+    };
     const size_t need = bytes;
     if (bytes < 2 * x.bytes) bytes = 2 * x.bytes;
-    e = hipMalloc(&p, bytes);
-    if (e != hipSuccess && bytes > need) {
-        (void)hipGetLastError();                 // handled here: not the next launch's
-        e = hipMalloc(&p, bytes = need);
-    }
+    e = allocate(bytes);
+    if (e != hipSuccess && bytes > need) e = allocate(bytes = need);
     if (e != hipSuccess) return e;
     x.ptr = p;                                   // a replaced buffer stays allocated
     x.bytes = bytes;

@@ -64,3 +64,10 @@ def test_room_for_the_call_but_not_for_twice_the_last(counter):
     assert [s for s, *_ in got] == [0, 0] and got[1][2] == sum(need)
     short = counter([f"memory {sum(need) - 4096}", a, b])
     assert short[0][0] == 0 and short[1][0] != 0
+
+
+def test_a_call_without_room_does_not_spoil_the_next(counter):
+    """Its error is its own status and not what the next call's launches find."""
+    a, b = fp8_call(100, 25600, 8192, "linear"), fp8_call(1100, 25600, 8192, "linear")
+    room = counter([a])[0][2]
+    assert [s == 0 for s, *_ in counter([f"memory {room + 4096}", a, b, a])] == [True, False, True]
