@@ -365,13 +365,13 @@ __global__ __launch_bounds__(64) void norm_cols_kernel(const T* __restrict__ x, 
 }
 
 // dw and db from the rows of partials: 16 waves take every 16th row of 64
-// columns, then add up in order.
+// columns, then add up in order; c0: the launch's first column.
 template <typename P>
-__global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict__ part, int n, int64_t C,
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict__ part, int n, int64_t c0, int64_t C,
                                                         P* __restrict__ dw, P* __restrict__ db) {
     __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t c = c0 + (int64_t)blockIdx.x * 64 + lane;
     P* const out = blockIdx.y == 0 ? dw : db;
     if (out == nullptr) return;
     float v = 0.0f;
@@ -393,6 +393,7 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict_
 
 constexpr int64_t kRegCols = 24576;              // the longest row held in registers
 constexpr int kMaxParts = 256;
+constexpr int64_t kMaxSumGrid = 1 << 21;
 
 // Element type of the parameters: x's own or fp32.
 template <typename F>
@@ -513,9 +514,14 @@ hipError_t launch_norm_grad(DType type, const void* x_, const void* dy_, int64_t
             }
         }
         if (e != hipSuccess || !sums) return e;
-        hipLaunchKernelGGL((norm_sum_kernel<P>), dim3((unsigned)((C + 63) / 64), 2), dim3(1024), 0, s, part, parts, C,
-                           (P*)dw, (P*)db);
-        return hipGetLastError();
+        // (a launch takes fewer than 2^32 work-items)
+        for (int64_t c0 = 0; c0 < C && e == hipSuccess; c0 += 64 * kMaxSumGrid) {
+            const int64_t left = (C - c0 + 63) / 64;
+            hipLaunchKernelGGL((norm_sum_kernel<P>), dim3((unsigned)(left < kMaxSumGrid ? left : kMaxSumGrid), 2),
+                               dim3(1024), 0, s, part, parts, c0, C, (P*)dw, (P*)db);
+            e = hipGetLastError();
+        }
+        return e;
     });
 }
 
