@@ -27,12 +27,6 @@
 namespace ue5m3 {
 namespace {
 
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
-    return (uint64_t)(uint32_t)uniform((int)(uint32_t)(v >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)v);
-}
-
 constexpr int kTile = 128, kRowBytes = 128;
 
 // Output tiles of 64 WM x 128, 2 WM waves of 64 x 64 (WM = 2 or 4), a ring of
@@ -49,26 +43,6 @@ struct Tile {
     static constexpr int kLoads = 5 + kLoadsB;
     static constexpr int kGroup = WM == 2 ? 8 : 4;   // tile rows, see tile_of()
 };
-
-// Direct loads to LDS that cost one instruction each: m0 holds the LDS address,
-// and the immediate offset counts for both sides (so a lane's source offset is
-// less by it).  The instructions between a write of m0 and a load that takes it
-// are the callers' matter: a wait state is needed there.
-__device__ __forceinline__ void set_m0(uint32_t lds) { asm volatile("s_mov_b32 m0, %0" :: "s"(lds) : "memory", "m0"); }
-
-template <int OFF>
-__device__ __forceinline__ void dma_rows(i32x4_t rsrc, uint32_t voff, uint32_t soff) {
-    asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" :: "v"(voff), "s"(rsrc), "s"(soff), "n"(OFF) : "memory");
-}
-
-// One dword (E8: byte) a lane to LDS at m0 + 4 lane.
-template <bool E8>
-__device__ __forceinline__ void dma_scale(i32x4_t rsrc, uint32_t voff) {
-    if (E8)
-        asm volatile("buffer_load_ubyte %0, %1, 0 offen lds" :: "v"(voff), "s"(rsrc) : "memory");
-    else
-        asm volatile("buffer_load_dword %0, %1, 0 offen lds" :: "v"(voff), "s"(rsrc) : "memory");
-}
 
 // One product from zero, into registers that a VALU instruction can read (the
 // compiler's own choice are accumulation registers, from where each value is
@@ -159,17 +133,17 @@ __global__ __launch_bounds__(128 * WM, 1) void gemm_fp8_kernel(int64_t M, int64_
                              (uint64_t)(tile_scale ? (int64_t)tn * KB + kb0 : kb0 * scale_pitch(rows) + x0) * kEl);
     const uint32_t srow =
         tile_scale ? 0u : (uint32_t)min((int64_t)(64 * (isA ? wave : wave & 1) + lane), rows - x0 - 1) * kEl;
-    // step i of stage kb's loads (8 rows each, at last the scales); m0 is written a
-    // step before the load that takes it
+    // step i of stage kb's loads (8 rows each, at last the scales)
     auto load = [&](auto ic, int kb, int slot) {
         constexpr int i = decltype(ic)::value;
-        if constexpr (i < kLoads - 1) dma_rows<(i & 3) * 1024>(i < 4 ? srcA : srcB, voff[i], (uint32_t)kb * 128u);
-        else {
-            dma_scale<E8>(i32x4_t{(int)(uint32_t)sat, (int)(uint32_t)(sat >> 32), (int)(L::kM * kEl), 0x00020000}, srow);
+        const uint32_t to = (uint32_t)(slot * kStageAll);
+        if constexpr (i < kLoads - 1) {
+            dma_rows<(i & 3) * 1024>(i < 4 ? srcA : srcB, voff[i], (uint32_t)kb * 128u, (i < 4 ? lds : lds_b) + to);
+        } else {
+            dma_scale<E8>(i32x4_t{(int)(uint32_t)sat, (int)(uint32_t)(sat >> 32), (int)(L::kM * kEl), 0x00020000}, srow,
+                          lds_s + to);
             sat += kb + 1 < kb1 ? sstep : 0;
         }
-        if constexpr (i == 3) set_m0(lds_b + (uint32_t)(slot * kStageAll));
-        if constexpr (i == kLoads - 2) set_m0(lds_s + (uint32_t)(slot * kStageAll));
     };
     using F = Frag<E8, TILED>;
     // Half h of a lane's 32 bytes of row group i: chunks g and g + 4 of eight,
@@ -227,7 +201,6 @@ __global__ __launch_bounds__(128 * WM, 1) void gemm_fp8_kernel(int64_t M, int64_
     // products later, when it has left the matrix pipe (at least 14 instructions
     // after its own, whatever else stands between them).
     auto turn = [&](F& f, F& n, int slot, int kb, int to) __attribute__((always_inline)) {
-        set_m0(lds + (uint32_t)(to * kStageAll));
         if (TILED && !E8) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) f.sa[i] *= f.st;
@@ -272,14 +245,8 @@ __global__ __launch_bounds__(128 * WM, 1) void gemm_fp8_kernel(int64_t M, int64_
     // waits count the same loads in every turn
     if (n > 0) {
 #pragma unroll
-        for (int k = 0; k < kRing; ++k) {
-            set_m0(lds + (uint32_t)(k * kStageAll));
-            asm volatile("s_nop 0");
-            static_for<0, kLoads>([&](auto ic) {
-                load(ic, min(kb0 + k, kb1 - 1), k);
-                asm volatile("s_nop 0");
-            });
-        }
+        for (int k = 0; k < kRing; ++k)
+            static_for<0, kLoads>([&](auto ic) { load(ic, min(kb0 + k, kb1 - 1), k); });
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads * (kRing - 1)) : "memory");
         F f, h;
         read_scales(f, 0);

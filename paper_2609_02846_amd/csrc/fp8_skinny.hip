@@ -41,27 +41,6 @@ struct SkinnyArgs {
     int M, K, KB;
 };
 
-__device__ __forceinline__ void set_m0(uint32_t lds) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" :: "s"(lds) : "memory", "m0"); }
-
-// 16 bytes a lane to LDS at m0 + OFF + 16 lane; OFF counts for the source too.
-template <int OFF>
-__device__ __forceinline__ void dma_rows(i32x4_t rsrc, uint32_t voff, uint32_t soff) {
-    asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" :: "v"(voff), "s"(rsrc), "s"(soff), "n"(OFF) : "memory");
-}
-
-// One dword (E8: byte) a lane to LDS at m0 + OFF + 4 lane, from voff + OFF.
-template <bool E8, int OFF>
-__device__ __forceinline__ void dma_scale(i32x4_t rsrc, uint32_t voff) {
-    if (E8)
-        asm volatile("buffer_load_ubyte %0, %1, 0 offen offset:%2 lds" :: "v"(voff), "s"(rsrc), "n"(OFF) : "memory");
-    else
-        asm volatile("buffer_load_dword %0, %1, 0 offen offset:%2 lds" :: "v"(voff), "s"(rsrc), "n"(OFF) : "memory");
-}
-
-__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32)) << 32 |
-           (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
-}
 __device__ __forceinline__ i32x4_t rsrc_of(uint64_t at, uint32_t bytes) {
     return i32x4_t{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
 }
@@ -117,24 +96,18 @@ __global__ __launch_bounds__(64 * NW) void gemm_fp8_skinny_kernel(const SkinnyAr
         bsat = uniform64(bs + (uint64_t)(TILED ? n0 / 128 * KB : n0) * kEl);
     };
     auto load = [&](int slot) {                  // the cursor's block, and on
-        set_m0(lds + (uint32_t)(slot * kStage));
-        const uint32_t so = (uint32_t)lb * 128u;
-        dma_rows<0>(srcB, voff, so);
-        dma_rows<1024>(srcB, voff + half, so);
+        const uint32_t so = (uint32_t)lb * 128u, to = lds + (uint32_t)(slot * kStage);
+        dma_rows<0>(srcB, voff, so, to);
+        dma_rows<1024>(srcB, voff + half, so, to);
         if (!FUSED) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
-                set_m0(lds + (uint32_t)(slot * kStage) + 2048u + t * 2048u);
-                dma_rows<0>(srcA, voff + t * 16u * Kp, so);
-                dma_rows<1024>(srcA, voff + t * 16u * Kp + half, so);
+                dma_rows<0>(srcA, voff + t * 16u * Kp, so, to + 2048u + t * 2048u);
+                dma_rows<1024>(srcA, voff + t * 16u * Kp + half, so, to + 2048u + t * 2048u);
             }
         }
-        set_m0(lds + (uint32_t)(slot * kStage) + kScaleB);
-        dma_scale<E8, 0>(rsrc_of(bsat + (uint64_t)lb * (TILED ? kEl : pb), 64 * kEl), brow);
-        if (!FUSED) {
-            set_m0(lds + (uint32_t)(slot * kStage) + kScaleA);
-            dma_scale<E8, 0>(rsrc_of(as + (uint64_t)lb * pa, 64 * kEl), arow);
-        }
+        dma_scale<E8>(rsrc_of(bsat + (uint64_t)lb * (TILED ? kEl : pb), 64 * kEl), brow, to + kScaleB);
+        if (!FUSED) dma_scale<E8>(rsrc_of(as + (uint64_t)lb * pa, 64 * kEl), arow, to + kScaleA);
         if (lb + NW < KB) {
             lb += NW;
         } else if (lt + grid < tiles) {          // past the last block the cursor stays on it

@@ -43,24 +43,6 @@ __device__ __forceinline__ void accumulate(f32x16& d, const i32x8& b, const i32x
                      : "+a"(d) : "v"(b), "v"(a), "v"(sb), "v"(sa));
 }
 
-__device__ __forceinline__ void set_m0(uint32_t lds) { asm volatile("s_mov_b32 m0, %0" :: "s"(lds) : "memory", "m0"); }
-
-// 16 bytes a lane to LDS at m0 + OFF + 16 lane; OFF counts for the source too.
-template <int OFF>
-__device__ __forceinline__ void dma_rows(i32x4_t rsrc, uint32_t voff, uint32_t soff) {
-    asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" :: "v"(voff), "s"(rsrc), "s"(soff), "n"(OFF) : "memory");
-}
-
-// One byte a lane, as a dword, to LDS at m0 + 4 lane.
-__device__ __forceinline__ void dma_code(i32x4_t rsrc, uint32_t voff) {
-    asm volatile("buffer_load_ubyte %0, %1, 0 offen lds" :: "v"(voff), "s"(rsrc) : "memory");
-}
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
-    return (uint64_t)(uint32_t)uniform((int)(uint32_t)(v >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)v);
-}
-
 template <int AF, bool TILED, bool OUT_BF16>
 __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_t N, int KB, int tiles_m, int tiles_n,
                                                                const uint8_t* __restrict__ A,
@@ -118,23 +100,23 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
             enter(++lk);
         }
     };
-    // step i of the cursor's stage into buffer b; m0 is written a step before
-    // the load that takes it
+    // step i of the cursor's stage into buffer b
     auto load = [&](auto ic, int b) {
         constexpr int i = decltype(ic)::value;
         if constexpr (i < 16) {
+            // (dma_rows(), with the sum in the place of its wait state)
             uint32_t vo;
-            asm volatile("v_add_u32 %0, %1, %2" : "=v"(vo) : "s"((uint32_t)i * 8u * Kp - (i & 3) * 1024u), "v"(voff));
-            dma_rows<(i & 3) * 1024>(src, vo, (uint32_t)lb * 128u);
-            if constexpr (i == 15) set_m0(lds_c + (uint32_t)(b * kScale));
-            else if constexpr (i % 4 == 3) set_m0(lds + (uint32_t)(b * kStage) + (i + 1) * 1024u);
+            asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\tbuffer_load_dwordx4 %0, %4, %5 offen offset:%6 lds"
+                         : "=&v"(vo) : "s"(lds + (uint32_t)(b * kStage) + (i & 12) * 1024u),
+                           "s"((uint32_t)i * 8u * Kp - (i & 3) * 1024u), "v"(voff), "s"(src), "s"((uint32_t)lb * 128u),
+                           "n"((i & 3) * 1024) : "memory", "m0");
         } else {
             uint32_t row;                            // the lane's, the last one past the operand's end
             asm volatile("v_add_u32 %0, %1, %2\n\tv_min_i32 %0, %3, %0"
                          : "=&v"(row) : "s"(half + 64 * (i - 16)), "v"(lane), "s"(cleft));
             if (tile_code) row = 0;
-            dma_code(i32x4_t{(int)(uint32_t)cat, (int)(uint32_t)(cat >> 32), 256, 0x00020000}, row);
-            if constexpr (i == 16) set_m0(lds_c + (uint32_t)(b * kScale) + 256u);
+            dma_scale<true>(i32x4_t{(int)(uint32_t)cat, (int)(uint32_t)(cat >> 32), 256, 0x00020000}, row,
+                            lds_c + (uint32_t)(b * kScale) + (i - 16) * 256u);
         }
     };
     // Lines of a later stage into the L2 (and to LDS that nobody reads): the eight
@@ -154,7 +136,8 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
         frow = (uint32_t)min(share, rows - x0 - 1) * Kp;
     };
     auto ahead = [&]() {
-        asm volatile("buffer_load_dword %0, %1, %2 offen lds" :: "v"(frow), "s"(fsrc), "s"((uint32_t)fb * 128u) : "memory");
+        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dword %0, %1, %2 offen lds"
+                     :: "v"(frow), "s"(fsrc), "s"((uint32_t)fb * 128u), "s"(lds_d) : "memory", "m0");
         if (fb + 1 < KB) {
             ++fb;
         } else if (fk + 1 < nw) {
@@ -163,7 +146,6 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
             enter_ahead();
         }
     };
-    auto start = [&](int b) { set_m0(lds + (uint32_t)(b * kStage)); };
 
     // ---- fragments ----------------------------------------------------------
     // offset of chunk c of slice s in a lane's first row of operand `op`: chunk
@@ -202,27 +184,15 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
     enter(0);
     enter_ahead();
     fb = min(1 + kAhead, KB - 1);
-    start(0);
-    asm volatile("s_nop 0");
-    static_for<0, 18>([&](auto ic) {
-        load(ic, 0);
-        asm volatile("s_nop 0");
-    });
+    static_for<0, 18>([&](auto ic) { load(ic, 0); });
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     static_for<0, 16>([&](auto qc) { read(qc, R0, 0, 0); });
 #pragma unroll
     for (int g = 0; g < 8; ++g) sc[g] = code(g, 0);
     advance();
-    start(1);
-    asm volatile("s_nop 0");
-    static_for<0, 18>([&](auto ic) {
-        load(ic, 1);
-        asm volatile("s_nop 0");
-    });
+    static_for<0, 18>([&](auto ic) { load(ic, 1); });
     // (as in every turn: the first one's wait leaves one load out, and the last code
     // of stage 1 must not be that one)
-    set_m0(lds_d);
-    asm volatile("s_nop 0");
     ahead();
 
     int b = 0;
@@ -254,18 +224,13 @@ __global__ __launch_bounds__(256, 1) void gemm_fp8_wide_kernel(int64_t M, int64_
             asm volatile("s_waitcnt vmcnt(1) lgkmcnt(0)\n\ts_barrier" ::: "memory");
             const int bn = b ^ 1;
             advance();
-            start(b);
             // slice 1, the next stage's slice 0 and codes and the loads of the one after
             static_for<0, 16>([&](auto qc) {
                 constexpr int q = decltype(qc)::value, i = q / 4, j = q % 4;
                 accumulate<AF>(acc[i][j], R1.v[4 + j], R1.v[i], sc[4 + j], sc[i]);
                 if constexpr (q < 2) load(std::integral_constant<int, 2 * q>{}, b);
                 load(std::integral_constant<int, q < 2 ? 2 * q + 1 : q + 2>{}, b);
-                if constexpr (q == 15) {
-                    set_m0(lds_d);
-                    asm volatile("s_nop 0");
-                    ahead();
-                }
+                if constexpr (q == 15) ahead();
                 read(qc, R0, 0, bn);
                 if constexpr (q < 8) scn[q] = code(q, bn);
                 __builtin_amdgcn_sched_barrier(0);
