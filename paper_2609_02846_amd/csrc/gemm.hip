@@ -1254,13 +1254,13 @@ __global__ __launch_bounds__(kGemmThreads, 1) void gemm_mx_kernel(
     // payload load i of the cursor's stage into buffer b
     auto load = [&](auto ic, int b) {
         constexpr int i = decltype(ic)::value;
-        dma_buf_x4<i * 1024>(pay, ls.off + i * 8 * rowb, (uint32_t)ls.g * kSupRowBytes,
-                             P0 + (uint32_t)(b * kSupPayload));
+        dma_buf_x4<i * 1024, !VEC>(pay, ls.off + i * 8 * rowb, (uint32_t)ls.g * kSupRowBytes,
+                                   P0 + (uint32_t)(b * kSupPayload));
     };
     auto load_scales = [&]() {
         const uint32_t at = (uint32_t)(ls.g >> 1) * 16u, to = S0 + (uint32_t)(lsb * kMxScl);
-        dma_buf_x4<0>(sca, ls.so[0] + at, 0u, to);
-        dma_buf_x4<1024>(sca, ls.so[1] + at, 0u, to);
+        dma_buf_x4<0, !VEC>(sca, ls.so[0] + at, 0u, to);
+        dma_buf_x4<1024, !VEC>(sca, ls.so[1] + at, 0u, to);
     };
     // one stage on, with the scales of the pair of stages it enters
     auto advance = [&]() {

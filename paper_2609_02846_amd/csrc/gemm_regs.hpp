@@ -88,11 +88,13 @@ __device__ __forceinline__ i32x4_t buffer_rsrc(const void* base, uint32_t bytes)
 
 // 16 bytes per lane from rsrc at voff + soff into LDS at lds + OFF + 16 lane
 // (the LDS offset is added inside the instruction sequence so that the
-// compiler does not keep one register per destination).
-template <int OFF>
+// compiler does not keep one register per destination).  SPILLED: for kernels
+// that run out of scalar registers and read the descriptor back from a vector
+// register's lanes: the load may take it five states later.
+template <int OFF, bool SPILLED = false>
 __device__ __forceinline__ void dma_buf_x4(i32x4_t rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
-    asm volatile("s_add_u32 m0, %3, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
-                 :: "v"(voff), "s"(rsrc), "s"(soff), "s"(lds), "i"(OFF) : "memory", "m0", "scc");
+    asm volatile("s_add_u32 m0, %3, %4\n\ts_nop %5\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+                 :: "v"(voff), "s"(rsrc), "s"(soff), "s"(lds), "i"(OFF), "i"(SPILLED ? 3 : 0) : "memory", "m0", "scc");
 }
 
 // vmcnt(n) with expcnt and lgkmcnt left at their maxima (n < 64).
