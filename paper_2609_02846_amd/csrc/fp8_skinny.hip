@@ -1,5 +1,6 @@
 // The 8-bit product for few rows of A (up to 64: tokens being decoded): every
-// weight is read once, so this is as fast as HBM gives B.
+// weight is read once, so this is as fast as HBM gives B.  The products are the
+// instruction of the 128 x 128 tiles, which truncates (see fp8_gemm.hip).
 //
 // A workgroup takes 16 rows of B at a time and splits the contraction over its
 // waves.  Each wave streams its own blocks through a ring of stages in LDS: whole

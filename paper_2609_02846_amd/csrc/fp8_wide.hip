@@ -4,7 +4,8 @@
 // Four waves of 128 x 128 accumulate in place in the accumulation registers,
 // with v_mfma_scale_f32_32x32x64_f8f6f4, which applies the scales: lane l
 // supplies row l % 32 and 32 of the 64 k of a slice, as two 16-byte chunks, and
-// its row's scale byte.  A stage is one block of 128 k, two slices; its 512 rows
+// its row's scale byte.  (It truncates small products next to large ones, as the
+// instruction of the smaller tiles does; see fp8_gemm.hip.)  A stage is one block of 128 k, two slices; its 512 rows
 // of 128 bytes lie in LDS with chunk c at c ^ (row % 8).  Workgroups are
 // persistent: the loads run two stages ahead over the stages of all of a
 // workgroup's tiles, so a tile's epilogue and the next one's start overlap them.

@@ -6,6 +6,8 @@ along each product's own contraction: X and dY along their rows and down their
 columns (both from one read), W in 128 x 128 tiles whose values the forward and
 the input gradient's product share.  X and W are E4M3, dY is E4M3 or E5M2
 (wider range).  Scales come from the blocks themselves, so there is no state.
+The outputs are bf16; the products' own arithmetic (see ue5m3_gemm_fp8) is 4e-5
+to 7e-5 from the exact sums in relative L2 norm, 1 / 24 of bf16's rounding.
 """
 
 import functools

@@ -246,7 +246,9 @@ def gemm_fp8(layout, M, N, K, a, a_scales, b, b_scales, out=None, out_dtype=torc
     the contraction (see ue5m3_gemm_fp8); layout is "nt", "nn" or "tn" as for
     ``gemm``.  ``a`` E4M3 or E5M2, ``b`` E4M3; ``a_blk`` / ``b_blk`` "row",
     "colT" or "tile" (None: activations and gradients 1D, weights in tiles, as
-    each product of a linear layer has them)."""
+    each product of a linear layer has them).  The matrix instructions truncate
+    small products next to large ones, at 2^-13 of those: fp32 output is 4e-5 to
+    7e-5 from the exact sum in relative L2 norm on normal values."""
     lay = _LAYOUTS[layout] if isinstance(layout, str) else int(layout)
     M, N, K = int(M), int(N), int(K)
     a_blk = ("colT" if lay == TN else "row") if a_blk is None else a_blk
@@ -273,7 +275,7 @@ def gemm_fp8(layout, M, N, K, a, a_scales, b, b_scales, out=None, out_dtype=torc
 def linear_fp8(x, w, w_scales, out=None, out_dtype=torch.bfloat16, stream=None):
     """Serving call: ``x`` [..., K] (bf16) times a weight [N, K] quantized once
     by ``quantize_fp8_tiles`` (``w`` [N, pad(K)], ``w_scales``); see
-    ue5m3_linear_fp8.  Returns [..., N]."""
+    ue5m3_linear_fp8.  Returns [..., N], with ``gemm_fp8``'s arithmetic."""
     _tensor(x, "x", (torch.bfloat16,))
     _tensor(w, "w", (torch.float8_e4m3fn,), x, 2)
     _tensor(w_scales, "w_scales", _SCALE_CODES, x, 2)
