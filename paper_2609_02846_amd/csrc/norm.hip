@@ -10,13 +10,15 @@
 // a lane), so the variance is the sum of squared distances from the mean that
 // is already known, and the backward pass reads each tensor once.
 //
-// Bound: HBM.  The backward pass's column sums stay in registers too, over all
-// the rows that a workgroup takes; each workgroup then writes one row of
-// partial sums, and a second kernel adds those rows in order, so the result
-// does not depend on which workgroup ended first.
+// Bound: HBM.  The backward pass's column sums stay in registers too (rows of up
+// to 8192), over all the rows that a workgroup takes; each workgroup then writes
+// one row of partial sums, and a second kernel adds those rows in order, so the
+// result does not depend on which workgroup ended first.
 //
-// 8192 x 4096 bf16 out of HBM: forward 31 us (4.3 TB/s), backward 52 us (3.9
+// 8192 x 4096 bf16 out of HBM: forward 32 us (4.2 TB/s), backward 52 us (3.9
 // TB/s) and its sum 4; a large copy reaches 5.2 TB/s.  One row: 3 us of kernel.
+// Longer rows, backward with its sum: 8192 x 16384 301 us (2.7 TB/s), 2000 x 21504
+// 100 (2.6).
 #include "io.hpp"
 
 namespace ue5m3 {
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* __restrict_
     out[c] = (P)v;
 }
 
-constexpr int64_t kRegCols = 24576;              // the longest row held in registers
+constexpr int64_t kRegCols = 24576, kBwdRegCols = 8192;   // the longest row held in registers
 constexpr int kMaxParts = 256;
 constexpr int64_t kMaxSumGrid = 1 << 21;
 
@@ -447,11 +449,14 @@ hipError_t launch_norm(DType type, const void* x_, int64_t rows, int64_t C, DTyp
         const P *w = (const P*)w_, *b = (const P*)b_;
         T* y = (T*)y_;
         // Waves a row and vectors a lane.  Many rows: as few waves as hold a row
-        // without many registers (8192 rows, us: C = 1024 1 x 2 8.5, 2 x 1 9.7; 2048
-        // 2 x 2 14.7, 4 x 1 16.4, 1 x 4 16.1; 4096 4 x 2 24, 8 x 1 32, 2 x 4 29; 8192
-        // 8 x 2 45, 4 x 4 51, 16 x 1 82).  Where the workgroups are fewer than the
-        // CUs twice over, latency: twice the waves (64 rows: 1024 3.2 against 3.5, 2048
-        // 3.2 against 3.6, 4096 3.3 against 3.7).
+        // without many registers (8192 rows out of HBM, us: C = 1024 1 x 2 9.8, 2 x 1
+        // 10.9; 2048 2 x 2 16.9, 4 x 1 17.8, 1 x 4 17.9; 4096 4 x 2 29, 8 x 1 36, 2 x 4
+        // 32; 8192 8 x 2 58, 4 x 4 57, 16 x 1 99).  Where the workgroups are fewer than
+        // the CUs twice over, latency: twice the waves, worth little (64 rows: 1024 4.64
+        // against 4.76, 4096 4.60, 4.68; 512 rows of 4096 5.1, 5.2).  From 8193 columns on
+        // the whole workgroup; against the streaming form it is the faster one for few
+        // rows and not for many: 256 rows of 12288 6.3, 6.9, of 21504 9.1, 9.7; 4096
+        // rows 67, 58 and 95, 95.
         const bool few = rows <= 512;
         if (C < 8) return fwd_l<T, P, 1, 1, Len::Tiny>(x, rows, C, w, b, eps, y, mean, rstd, s);
         if (C <= 512) return fwd<T, P, 1, 1>(x, rows, C, w, b, eps, y, mean, rstd, s);
@@ -480,14 +485,16 @@ hipError_t launch_norm_grad(DType type, const void* x_, const void* dy_, int64_t
         const P* w = (const P*)w_;
         T* dx = (T*)dx_;
         const bool sums = dw != nullptr || db != nullptr;
-        // Waves a row, one vector a lane as long as that goes (8192 rows, us, with the
-        // sum: C = 1024 2 x 1 19, 1 x 2 23; 4096 8 x 1 45, 4 x 2 47, 2 x 4 188, whose
-        // registers spill; 8192 16 x 1 102, 8 x 2 110), and how many workgroups of 1024
-        // threads take the rows.
+        // Waves a row, one vector a lane (8192 rows out of HBM, us, with the sum: C =
+        // 1024 2 x 1 21, 1 x 2 25; 4096 8 x 1 53, 4 x 2 54, 2 x 4 184, whose registers
+        // spill; 8192 16 x 1 101, 8 x 2 110), and how many workgroups of 1024 threads
+        // take the rows.  Longer rows would take two vectors a lane of 16 waves, which
+        // spill, and are streamed (2 and 3 vectors against the streaming form: 1 x 8200
+        // 21.9, 9.3; 4096 x 8200 147, 99; 8192 x 16384 403, 301; 2000 x 21504 260, 100).
         const int nw = C <= 512 ? 1 : C <= 1024 ? 2 : C <= 2048 ? 4 : C <= 4096 ? 8 : 16;
         const int64_t groups = (rows + 16 / nw - 1) / (16 / nw);
         int parts = (int)(groups < kMaxParts ? groups : kMaxParts);
-        if (C > kRegCols) parts = (int)(rows < 64 ? rows : 64);
+        if (C > kBwdRegCols) parts = (int)(rows < 64 ? rows : 64);
         if (parts < 1) parts = 1;                    // no rows: sums of nothing
         Workspace held;
         float* part = nullptr;
@@ -499,9 +506,7 @@ hipError_t launch_norm_grad(DType type, const void* x_, const void* dy_, int64_t
         else if (C <= 1024) e = bwd<T, P, 2, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
         else if (C <= 2048) e = bwd<T, P, 4, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
         else if (C <= 4096) e = bwd<T, P, 8, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
-        else if (C <= 8192) e = bwd<T, P, 16, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
-        else if (C <= 16384) e = bwd<T, P, 16, 2>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
-        else if (C <= kRegCols) e = bwd<T, P, 16, 3>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
+        else if (C <= kBwdRegCols) e = bwd<T, P, 16, 1>(x, dy, rows, C, w, mean, rstd, res, dx, part, parts, s);
         else {
             if (dx != nullptr && rows > 0)
                 hipLaunchKernelGGL((norm_bwd_long_kernel<T, P>), dim3((unsigned)(rows < (1 << 20) ? rows : (1 << 20))),
