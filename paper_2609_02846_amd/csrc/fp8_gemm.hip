@@ -21,9 +21,9 @@
 // against as many of the loads (32 KB at 64 bytes a cycle) and of LDS reads (64 KB at
 // 128), with one wave a SIMD to issue all of it: about 1270 cycles a block.  The
 // 256 x 128 tiles halve the loads of B, and two waves a SIMD fill each other's gaps:
-// under F32 scales 8192^3 497 us (2210 TFLOP/s; 128 x 128 585), 8192 x 4096 x 21504 640
-// (784); under E8M0 2000 x 4096 x 4096 32 (36.5).  The small tiles stay for
-// products of few tiles: 1999 x 1360 x 3408 17.6, the large 24.
+// out of HBM, under F32 scales 8192^3 495 us (2220 TFLOP/s; 128 x 128 623), 8192 x
+// 4096 x 21504 631 (778); under E8M0 2000 x 4096 x 4096 34 (43).  The small tiles
+// stay for products of few tiles: 1999 x 1360 x 3408 F32 20, the large 29.
 #include <algorithm>
 
 #include "fp8.hpp"
@@ -42,6 +42,8 @@ constexpr int kTile = 128, kRowBytes = 128;
 // barrier that opens turn k, stage k + 1 has landed and stage k has left the LDS,
 // so stage k + kRing takes its place.  Scales travel with their stage, one dword
 // for each row (an E8M0 byte is loaded as one).
+// (WM = 4 under one-dimensional F32 scales spills three or four registers, before
+// and after the loop's full turns; what is read back makes a wait there stricter.)
 template <int WM>
 struct Tile {
     static constexpr int kM = 64 * WM, kThreads = 128 * WM, kRing = WM == 2 ? 4 : 3;
@@ -366,12 +368,14 @@ struct Plan {
 
 // The fastest by modelled times in us: rounds of one tile a CU, each with a fixed
 // part and one for each block, and for split tiles the sum's launch and the
-// partial sums' way out and back.  Model / measured on 256 CUs, M x N x K (F32: 128,
-// 256 rows; E8M0: 128, 256, wide):
-//   8192 x 21504 x 4096   F32 908 / 913, 706 / 707    E8M0 881 / 878, 649 / 655, 588 / 570
-//   2000 x 4096 x 4096    F32 43 / 43, 34 / 38        E8M0 42 / 36, 31 / 33, 53 / 56
-//   777 x 4096 x 21504    F32 98 / 96, 99 / 97        E8M0 94 / 84, 88 / 88, 257 / -
-//   1999 x 1360 x 3408    F32 19 / 18, 23 / 25        E8M0 18 / 16, 23 / 24, 46 / -
+// partial sums' way out and back.  Model / measured on 256 CUs out of HBM, M x N x K
+// (F32: 128, 256 rows; E8M0: 128, 256, wide):
+//   8192 x 21504 x 4096   F32 908 / 914, 706 / 713    E8M0 881 / 882, 650 / 655, 588 / 568
+//   8192 x 4096 x 21504   F32 782 / 778, 635 / 631    E8M0 755 / 757, 543 / 563, 515 / 517
+//   2000 x 4096 x 4096    F32 43 / 45, 34 / 37        E8M0 42 / 43, 31 / 34, 54 / 49
+//   777 x 4096 x 21504    F32 98 / 99, 99 / 94        E8M0 94 / 97, 88 / 88, 258 / 211
+//   1999 x 1360 x 3408    F32 19 / 20, 29 / 29        E8M0 18 / 19, 27 / 27, 46 / 42
+//   1999 x 3408 x 1360    F32 20 / 24, 14 / 18        E8M0 19 / 23, 15 / 17, 22 / 25
 static hipError_t make_plan(int64_t M, int64_t N, int64_t K, bool e8, Plan& p) {
     const hipError_t err = device_cus(&p.cus);
     if (err != hipSuccess) return err;

@@ -21,9 +21,9 @@
 // whole 128-byte rows.  Rows alone need no tile: their kernel gives a block to
 // 16 lanes, so that few rows still spread over many waves.
 //
-// 8192 x 21504 both ways 144 us (4.9 TB/s; a large copy 5.2), 8192 x 4096 30 (4.5),
-// tiles with the transposed copy of 21504 x 4096 62 (5.7); 1999 x 3408 both ways 13.6
-// (2.0: 432 workgroups, a tile each, with nothing behind them).
+// 8192 x 21504 both ways 144 - 152 us (4.6 - 4.9 TB/s; a large copy 5.2), 8192 x 4096 30
+// (4.5), tiles with the transposed copy of 21504 x 4096 61 (5.8); 1999 x 3408 both ways
+// 14 - 15 (1.8 - 2.0: 432 workgroups, a tile each, with nothing behind them).
 #include "codec.hpp"
 #include "fp8.hpp"
 #include "io.hpp"

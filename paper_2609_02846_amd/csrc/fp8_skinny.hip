@@ -16,9 +16,9 @@
 // one launch, and nothing to wait for, instead of two (1 x 6144 x 4096 9.3 us, two
 // launches 11.5; 1 x 3408 x 1360 4.4 and 6.0; but 4 x 6144 x 4096 12.7 and 10.7).
 //
-// Out of HBM: 1 x 6144 x 4096 9.3 us (2.7 TB/s: a wave holds six blocks, and the
-// start and the sums are half of the time), 24 x 21504 x 4096 22 - 24 us (3.8 - 4.1
-// TB/s); a large copy reaches 5.2 TB/s.
+// Out of HBM: 1 x 6144 x 4096 9.4 - 10.3 us (2.5 - 2.7 TB/s: a wave holds six blocks,
+// and the start and the sums are half of the time), 24 x 21504 x 4096 24 - 27 us (3.3 -
+// 3.7 TB/s); a large copy reaches 5.2 TB/s.
 #include <algorithm>
 #include <atomic>
 

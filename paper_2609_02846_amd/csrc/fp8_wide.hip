@@ -9,14 +9,17 @@
 // of 128 bytes lie in LDS with chunk c at c ^ (row % 8).  Workgroups are
 // persistent: the loads run two stages ahead over the stages of all of a
 // workgroup's tiles, so a tile's epilogue and the next one's start overlap them.
+// (With fp32 output four registers spill over the K loop: to read them back at a
+// tile's end waits for every load, and that overlap is lost.)
 //
 // Bound: a CU takes in 64 KB for 2048 cycles of the matrix pipe, half of what
 // the 128 x 128 tiles need for as many products, which were held up there by
 // the loads (half of each wave's time it waited to issue one).  LDS reads and
 // loads stand between the products, one of each, so that neither comes in bursts.
-// 8192 x 21504 x 4096 530 - 615 us (2350 - 2720 TFLOP/s), 8192 x 4096 x 21504 525, 8192^3
-// 397 (2770; without the lines fetched ahead into L2 12% slower), where the
-// library's product under one scale for each tensor takes 393.
+// Out of HBM 8192 x 21504 x 4096 568 - 577 us (2500 - 2540 TFLOP/s; within a training
+// step 595 - 607), 8192 x 4096 x 21504 517 - 535, 8192^3 402 - 413 (2660 - 2730; without
+// the lines fetched ahead into L2 12% slower), where the library's product under
+// one scale for each tensor takes 393.
 #include "fp8.hpp"
 #include "fp8_tile.hpp"
 #include "gemm_regs.hpp"
