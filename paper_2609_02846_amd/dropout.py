@@ -45,7 +45,8 @@ class Dropout(torch.nn.Module):
     them drop the same elements, and the seeds of ranks have to be further
     apart than a run has calls.  A call inside a backward pass, where
     checkpointing repeats one, is refused then: which call it repeats the
-    count does not tell."""
+    count does not tell.  (A call captured in a graph holds its key: every replay
+    drops the same elements.)"""
 
     def __init__(self, p=0.1, seed=None, layer_id=0):
         super().__init__()
