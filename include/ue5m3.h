@@ -616,6 +616,201 @@ ue5m3_status_t ue5m3_linear_fp8(const void* x_bf16, int64_t T, int64_t K, int64_
                                 const void* w_scales, ue5m3_fp8_scale_t scale_kind, void* y, ue5m3_out_t y_type,
                                 hipStream_t stream);
 
+/*
+ * ------------------------------------------------------------------------
+ * Attention between a QKV projection and an output projection: the norms of
+ * queries and keys with the rotation by position, attention of ragged
+ * sequences with its gradients, attention of single tokens over a paged cache,
+ * and copies of the cache's pages.  Arguments come in structures, read before
+ * the call returns (zero what a call does not use).  Strides are in elements,
+ * the elements of a head lie together, and in every tensor heads do not
+ * overlap.  These calls use no library workspace: where one needs scratch
+ * memory the caller passes it (4-byte aligned, any contents), so none of them
+ * needs an earlier call before a capture, and graphs share no memory that
+ * their callers do not.
+ * ------------------------------------------------------------------------
+ */
+
+/*
+ * Queries q and keys k of `tokens` tokens: element d of head h of token t at
+ * t * (q_token or k_token) + h * (q_head or k_head) + d, any alignment of the
+ * type (bf16, fp16 or fp32), dim <= 256.  Of each head's row x:
+ *   norm != 0:  n = x r w, r = 1 / sqrt(sum(x^2) / dim + eps), w the dim elements of
+ *               q_weight or k_weight (null: 1) of weight_type, which is `type` or
+ *               UE5M3_F32; else n = x;
+ *   pairs > 0:  each of the pairs p < pairs <= dim / 2, (a, b) = (n[p], n[p + pairs])
+ *               or, interleaved != 0, (n[2 p], n[2 p + 1]), becomes
+ *               amplitude (a cos t - b sin t, a sin t + b cos t), t = position freqs[p]
+ *               (freqs in binary32, the angle in binary64, at least 2^-26 of a
+ *               turn); the elements past 2 pairs stay,
+ * in binary32, rounded once.  The position of token t is positions[t], or t % period
+ * where positions is null.
+ */
+typedef struct {
+    int64_t tokens;
+    int32_t q_heads, kv_heads, dim, pairs;
+    ue5m3_dtype_t type, weight_type;
+    int32_t norm, interleaved;
+    float eps, amplitude;
+    const void *q, *k;
+    int64_t q_token, q_head, k_token, k_head;
+    const void *q_weight, *k_weight;
+    const int64_t* positions;
+    int64_t period;
+    const float* freqs;
+    void *q_out, *k_out;             /* results (of the gradient call dq and dk) */
+    int64_t q_out_token, q_out_head, k_out_token, k_out_head;
+} ue5m3_rope_t;
+
+/*
+ * A cache of keys and values: token s of a page, head h, element d at
+ * n * page + s * token + h * head + d of k and of v, n < pages the page's number.
+ * page_size tokens a page, a power of two.
+ */
+typedef struct {
+    void *k, *v;
+    int64_t pages;
+    int32_t page_size;
+    int64_t page, token, head;
+} ue5m3_pages_t;
+
+/*
+ * q_out and k_out from q and k.  They may be q and k themselves (with their
+ * strides).  EINVAL: a bad type or flag, eps negative or not finite, an amplitude
+ * not finite, a null pointer that is needed (tokens > 0), no norm and no pairs, or
+ * period < 1 without positions; ESHAPE: a negative size, dim outside [1, 256],
+ * pairs above dim / 2, a head count below 1 (q) or 0 (k) or above 2^16, or too many
+ * tokens (2^40); EALIGN.
+ */
+ue5m3_status_t ue5m3_qk_norm_rope(const ue5m3_rope_t* args, hipStream_t stream);
+
+/*
+ * Its gradients: q_out and k_out of `args` receive dq and dk (nullable) for the
+ * output gradients dq_rotated [tokens][q_heads][dim] and dk_rotated
+ * [tokens][kv_heads][dim] (dense); dq and dk may be these themselves.  dq_weight and
+ * dk_weight [dim] (weight_type, nullable) are summed in binary32 in a fixed order
+ * through `scratch`, of ue5m3_qk_norm_rope_grad_scratch(tokens, q_heads + kv_heads,
+ * dim) bytes (null where neither is asked for); without norm they must be null.
+ */
+int64_t ue5m3_qk_norm_rope_grad_scratch(int64_t tokens, int32_t heads, int32_t dim);
+ue5m3_status_t ue5m3_qk_norm_rope_grad(const ue5m3_rope_t* args, const void* dq_rotated, const void* dk_rotated,
+                                       void* dq_weight, void* dk_weight, void* scratch, hipStream_t stream);
+
+/*
+ * The serving form: q_out as above; the keys, and the values v [tokens][kv_heads][dim]
+ * (with strides, of `type`), go to the cache instead (k_out is not used): those of
+ * token t to page slots[t] / page_size, place slots[t] % page_size.  A slot below 0
+ * or past the cache writes nothing (a padded batch's tokens).  Two tokens must not
+ * have one slot.  q_heads may be 0 here, and norm and pairs too (rows are copied).
+ * EINVAL also: page_size no power of two; ESHAPE: kv_heads 0.
+ */
+ue5m3_status_t ue5m3_qk_norm_rope_append(const ue5m3_rope_t* args, const void* v, int64_t v_token, int64_t v_head,
+                                         const ue5m3_pages_t* cache, const int64_t* slots, hipStream_t stream);
+
+/*
+ * Copies pages within each of `planes` planes at `base`, `plane` bytes apart, that hold
+ * `pages` pages of `page` bytes each, one after the other: page src[i] to dst[i] for
+ * i < n.  src and dst are HOST arrays, read before the call returns.  EINVAL: a page
+ * outside [0, pages), a page twice in dst or in both src and dst, a null pointer;
+ * ESHAPE: a negative size, pages that overlap the next plane, or `page` or `plane`
+ * odd; EALIGN: base odd.  Fast where base, plane and page are multiples of 16.
+ */
+ue5m3_status_t ue5m3_copy_pages(void* base, int64_t planes, int64_t plane, int64_t pages, int64_t page,
+                                const int32_t* src, const int32_t* dst, int64_t n, hipStream_t stream);
+
+/*
+ * Attention of `sequences` sequences: sequence i has queries q_starts[i] .. q_starts[i + 1]
+ * - 1 and keys (and values) k_starts[i] .. k_starts[i + 1] - 1, int32 device arrays of
+ * sequences + 1 numbers, from 0 or more, ascending, at most q_tokens and k_tokens (kept
+ * within them, whatever they hold); both null: equal shares of the tokens.  Query i of
+ * a sequence with L queries and S keys stands at position p = i + S - L, so that the
+ * last query has the last key.  It sees key j < S
+ *   causal == 0:  always;
+ *   causal != 0:  if j <= p, and, for window > 0, p - j < window or j < sinks.
+ *     o = sum over seen j of exp(s_j) v_j / sum of exp(s_j), s_j = scale (q . k_j),
+ * for q_heads query heads in groups of q_heads / kv_heads, one for each key-value
+ * head.  A query that sees nothing gives zeros.  Scores, sums and o are binary32; P
+ * (and, of the gradient, dS) is rounded to `type` (bf16 or fp16) for its product; o is
+ * rounded once.  What a query does not see has to be finite all the same within its
+ * sequence (it is multiplied by 0).  lse [q_heads][q_tokens] (nullable) receives log(sum
+ * of exp(s_j)), -inf for a query that sees nothing; o_rest (nullable, as o) what the
+ * rounding left, rounded to `type` itself: the gradients need more of o than it holds.
+ * Tokens of no sequence get zeros (lse -inf).  q, k and v have strides, o is dense
+ * [q_tokens][q_heads][dim].
+ *
+ * q, k, v, o and o_rest are 16-byte aligned, strides are multiples of 8 elements, dim is a
+ * multiple of 8 up to 128.  EINVAL: a type that is not bf16 or fp16, a scale that is
+ * not positive and finite, causal == 0 with a window, a null pointer; ESHAPE: a
+ * negative size, q_heads no multiple of kv_heads, sequences < 1, tokens above 2^30 or no
+ * multiple of `sequences` where q_starts is null, a token stride of 2^23 or more or below
+ * dim, more work than a launch takes; EALIGN.
+ */
+typedef struct {
+    int64_t q_tokens, k_tokens, sequences;
+    const int32_t *q_starts, *k_starts;
+    int32_t q_heads, kv_heads, dim;
+    ue5m3_dtype_t type;
+    int32_t causal;
+    float scale;
+    int64_t window, sinks;
+    const void *q, *k, *v;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;
+    void *o, *o_rest;
+    float* lse;
+} ue5m3_attention_t;
+
+ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, hipStream_t stream);
+
+/*
+ * Its gradients for the output gradient d_o (dense): with P = exp(s - lse) and
+ * delta = sum(d_o (o + o_rest)) of each row, dS = P (d_o . v - delta), dq = scale dS k,
+ * dk = scale dS^T q, dv = P^T d_o, the last two summed over the query heads that share
+ * a key-value head, in a fixed order.  `args` as of the forward call, with its o,
+ * o_rest and lse; delta [q_heads][q_tokens] is scratch that the call writes.  dq, or dk and dv
+ * together, may be null.  16-byte alignment and strides as for q, k and v.
+ */
+typedef struct {
+    const void* d_o;
+    float* delta;
+    void *dq, *dk, *dv;
+    int64_t dq_token, dq_head, dk_token, dk_head, dv_token, dv_head;
+} ue5m3_attention_grad_t;
+
+ue5m3_status_t ue5m3_attention_grad(const ue5m3_attention_t* args, const ue5m3_attention_grad_t* grad,
+                                    hipStream_t stream);
+
+/*
+ * Attention of one new token for each of `rows` sequences, over the pages that row
+ * i of table (int32, table_row apart, `width` numbers) names: with n = lengths[i] the
+ * token sees keys n - 1 (its own, written before) down to 0, of them under a window
+ * j >= n - window and j < sinks.  n <= 0 gives zeros.  A page number outside the cache
+ * that is needed, or n above width * page_size, makes the row NaN (nothing outside the
+ * cache is read); what lies in the cache past a sequence's end or out of its window is
+ * not read.  o is dense [rows][q_heads][dim]; types, alignment, arithmetic and errors as
+ * of ue5m3_attention (the cache's strides too are multiples of 8).  Sequences are
+ * worked on in parts, which meet in `scratch`, of ue5m3_paged_attention_scratch(rows,
+ * q_heads, kv_heads, dim, width * page_size, window, sinks) bytes (null where that is 0).
+ * width * page_size is at most 2^30.
+ */
+typedef struct {
+    int64_t rows;
+    int32_t q_heads, kv_heads, dim;
+    ue5m3_dtype_t type;
+    float scale;
+    int64_t window, sinks;
+    const void* q;
+    int64_t q_token, q_head;
+    ue5m3_pages_t cache;
+    const int32_t* table;
+    int64_t width, table_row;
+    const int32_t* lengths;
+    void* o;
+} ue5m3_paged_attention_t;
+
+int64_t ue5m3_paged_attention_scratch(int64_t rows, int32_t q_heads, int32_t kv_heads, int32_t dim, int64_t capacity,
+                                      int64_t window, int64_t sinks);
+ue5m3_status_t ue5m3_paged_attention(const ue5m3_paged_attention_t* args, void* scratch, hipStream_t stream);
+
 /* Static description of a status code. */
 const char* ue5m3_status_string(ue5m3_status_t status);
 

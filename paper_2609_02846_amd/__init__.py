@@ -39,6 +39,9 @@ EXPORTED_SYMBOLS = (
     "ue5m3_status_string", "ue5m3_version", "ue5m3_gemm_noalloc",
     "ue5m3_layer_norm", "ue5m3_layer_norm_grad", "ue5m3_dropout",
     "ue5m3_quantize_fp8", "ue5m3_quantize_fp8_tiles", "ue5m3_gemm_fp8", "ue5m3_linear_fp8",
+    "ue5m3_qk_norm_rope", "ue5m3_qk_norm_rope_grad", "ue5m3_qk_norm_rope_grad_scratch", "ue5m3_qk_norm_rope_append",
+    "ue5m3_copy_pages", "ue5m3_attention", "ue5m3_attention_grad", "ue5m3_paged_attention",
+    "ue5m3_paged_attention_scratch",
 )
 
 
@@ -46,6 +49,69 @@ class AmaxStateC(ctypes.Structure):
     """Mirror of ue5m3_amax_state_t."""
     _fields_ = [("amax_dev", ctypes.c_void_p), ("last_refresh", ctypes.c_int64),
                 ("period", ctypes.c_int32), ("has_cache", ctypes.c_int32)]
+
+
+def _fields(text):
+    """(name, type) of lines of a C structure: "i64 tokens"."""
+    kinds = {"p": ctypes.c_void_p, "i64": ctypes.c_int64, "i32": ctypes.c_int32, "f32": ctypes.c_float}
+    return [(n, kinds[line.split()[0]]) for line in text.strip().splitlines() for n in line.split()[1:]]
+
+
+class RopeC(ctypes.Structure):
+    """Mirror of ue5m3_rope_t."""
+    _fields_ = _fields("""
+        i64 tokens
+        i32 q_heads kv_heads dim pairs type weight_type norm interleaved
+        f32 eps amplitude
+        p q k
+        i64 q_token q_head k_token k_head
+        p q_weight k_weight positions
+        i64 period
+        p freqs q_out k_out
+        i64 q_out_token q_out_head k_out_token k_out_head""")
+
+
+class PagesC(ctypes.Structure):
+    """Mirror of ue5m3_pages_t."""
+    _fields_ = _fields("""
+        p k v
+        i64 pages
+        i32 page_size
+        i64 page token head""")
+
+
+class AttentionC(ctypes.Structure):
+    """Mirror of ue5m3_attention_t."""
+    _fields_ = _fields("""
+        i64 q_tokens k_tokens sequences
+        p q_starts k_starts
+        i32 q_heads kv_heads dim type causal
+        f32 scale
+        i64 window sinks
+        p q k v
+        i64 q_token q_head k_token k_head v_token v_head
+        p o o_rest lse""")
+
+
+class AttentionGradC(ctypes.Structure):
+    """Mirror of ue5m3_attention_grad_t."""
+    _fields_ = _fields("""
+        p d_o delta dq dk dv
+        i64 dq_token dq_head dk_token dk_head dv_token dv_head""")
+
+
+class PagedAttentionC(ctypes.Structure):
+    """Mirror of ue5m3_paged_attention_t."""
+    _fields_ = _fields("""
+        i64 rows
+        i32 q_heads kv_heads dim type
+        f32 scale
+        i64 window sinks
+        p q
+        i64 q_token q_head""") + [("cache", PagesC)] + _fields("""
+        p table
+        i64 width table_row
+        p lengths o""")
 
 
 class UE5M3Error(RuntimeError):
@@ -121,6 +187,25 @@ def load_library(path=LIB_PATH):
     lib.ue5m3_gemm_fp8.restype = i32
     lib.ue5m3_linear_fp8.argtypes = [vp, i64, i64, i64, vp, vp, i32, vp, i32, vp]
     lib.ue5m3_linear_fp8.restype = i32
+    ptr = ctypes.POINTER
+    lib.ue5m3_qk_norm_rope.argtypes = [ptr(RopeC), vp]
+    lib.ue5m3_qk_norm_rope.restype = i32
+    lib.ue5m3_qk_norm_rope_grad.argtypes = [ptr(RopeC), vp, vp, vp, vp, vp, vp]
+    lib.ue5m3_qk_norm_rope_grad.restype = i32
+    lib.ue5m3_qk_norm_rope_grad_scratch.argtypes = [i64, i32, i32]
+    lib.ue5m3_qk_norm_rope_grad_scratch.restype = i64
+    lib.ue5m3_qk_norm_rope_append.argtypes = [ptr(RopeC), vp, i64, i64, ptr(PagesC), vp, vp]
+    lib.ue5m3_qk_norm_rope_append.restype = i32
+    lib.ue5m3_copy_pages.argtypes = [vp, i64, i64, i64, i64, ptr(i32), ptr(i32), i64, vp]
+    lib.ue5m3_copy_pages.restype = i32
+    lib.ue5m3_attention.argtypes = [ptr(AttentionC), vp]
+    lib.ue5m3_attention.restype = i32
+    lib.ue5m3_attention_grad.argtypes = [ptr(AttentionC), ptr(AttentionGradC), vp]
+    lib.ue5m3_attention_grad.restype = i32
+    lib.ue5m3_paged_attention.argtypes = [ptr(PagedAttentionC), vp, vp]
+    lib.ue5m3_paged_attention.restype = i32
+    lib.ue5m3_paged_attention_scratch.argtypes = [i64, i32, i32, i32, i64, i64, i64]
+    lib.ue5m3_paged_attention_scratch.restype = i64
     lib.ue5m3_status_string.argtypes = [i32]
     lib.ue5m3_status_string.restype = ctypes.c_char_p
     lib.ue5m3_version.argtypes = []

@@ -1,0 +1,502 @@
+// Attention of ragged sequences, forward: of each query, the softmax over the keys
+// it sees times their values, in one pass over the keys with the running maximum
+// and sum.  Query i of a sequence of L queries and S keys stands at position
+// p = i + S - L; it sees key j when j <= p and, under a window, p - j < window or
+// j < sinks.  A row that sees nothing gives zeros.
+//
+// A workgroup of four waves takes 128 queries of a head, 32 a wave, and walks
+// through the keys 64 at a time.  Scores are computed transposed (keys x
+// queries), so that a lane has 32 scores of one query and P^T is the second
+// product's operand as it lies in its registers; the output is accumulated
+// transposed too.  P is rounded to the inputs' type, as the matrix instructions
+// take it; scores, sums and the output are binary32.
+#include <algorithm>
+
+#include "attention.hpp"
+#include "attn_tile.hpp"
+#include "io.hpp"
+
+namespace ue5m3 {
+namespace {
+
+constexpr int kAttnThreads = 256, kRows = 128, kKeys = 64;
+
+// The reference of a row's exponentials follows its maximum only where that has
+// grown by more than 2^8: until then P is at most 2^8, which loses nothing in
+// binary floating point, and the sums need no correction.
+constexpr float kSlack = 8.0f;
+
+struct Sight {                                       // what the rows of a sequence see
+    int keys, window, sinks;
+    bool causal;
+    // The keys j that position p sees: j <= last and (j > before or j < sinks).
+    __device__ __forceinline__ int last(int p) const { return causal ? min(p, keys - 1) : keys - 1; }
+    __device__ __forceinline__ int before(int p) const { return causal && window != 0 ? p - window : -1; }
+    // Whether rows at positions lo .. hi all see keys j .. j + n - 1, or none does.
+    __device__ __forceinline__ bool all(int lo, int hi, int j, int n) const {
+        return j + n <= keys && (!causal || (j + n - 1 <= lo && (window == 0 || hi - j < window || j + n <= sinks)));
+    }
+    __device__ __forceinline__ bool none(int lo, int hi, int j, int n) const {
+        return j >= keys || (causal && (j > hi || (window != 0 && lo - (j + n - 1) >= window && j >= sinks)));
+    }
+};
+
+// (selects without a branch)
+__device__ __forceinline__ bool seen(int j, int last, int before, int sinks) {
+    return (j <= last) & ((j > before) | (j < sinks));
+}
+
+// The key tiles that rows at positions lo .. hi see: `sinks` first ones, then those
+// from `from` on.
+struct KeyTiles {
+    int sinks, from, n;
+    __device__ __forceinline__ KeyTiles(const Sight& s, int lo, int hi) {
+        const int end = s.causal ? min(max(hi + 1, 0), s.keys) : s.keys;
+        from = s.causal && s.window != 0 ? max(0, lo - s.window + 1) / kKeys : 0;
+        const int to = (end + kKeys - 1) / kKeys;
+        sinks = min((min(s.sinks, end) + kKeys - 1) / kKeys, from);
+        n = sinks + max(0, to - from);
+    }
+    __device__ __forceinline__ int operator[](int i) const { return i < sinks ? i : from + i - sinks; }
+};
+
+__device__ __forceinline__ Sight sight(const ue5m3_attention_t& a, int keys) {
+    return Sight{keys, a.window < keys ? (int)a.window : 0, (int)min(a.sinks, (int64_t)keys), a.causal != 0};
+}
+
+// Head of work item id, so that the query heads of a key-value head meet on one XCD:
+// workgroups go round the eight.
+__device__ __forceinline__ int head_of(int id, int q_heads, int kv_heads) {
+    const int at = id % q_heads;
+    return at % kv_heads * (q_heads / kv_heads) + at / kv_heads;
+}
+
+// Lane l's operand of a row in global memory: elements 16 s + 8 h .., zeros past dim.
+template <int DT>
+__device__ __forceinline__ void load_operand(u32x4 (&f)[DT / 16], const void* row, int dim) {
+    const int h = (int)(threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int s = 0; s < DT / 16; ++s) {
+        f[s] = u32x4{0, 0, 0, 0};
+        if (16 * s + 8 * h < dim) __builtin_memcpy(&f[s], (const uint16_t*)row + 16 * s + 8 * h, 16);
+    }
+}
+
+// A transposed accumulator's column (a lane pair's row of the tensor) times f.
+template <typename T, int DT>
+__device__ __forceinline__ void store_column(T* row, const f32x16 (&o)[DT / 32], float f, int dim) {
+    const int h = (int)(threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int b = 0; b < DT / 32; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * b + 8 * g + 4 * h;
+            const u32x2 w = {pack2<T>(o[b][4 * g] * f, o[b][4 * g + 1] * f), pack2<T>(o[b][4 * g + 2] * f, o[b][4 * g + 3] * f)};
+            if (d < dim) __builtin_memcpy(row + d, &w, 8);
+        }
+}
+
+// Rows of no sequence: zeros in this head's share of an output (each workgroup past
+// the tiles takes every `extras`-th row), and -inf for `lse`.
+template <typename T>
+__device__ __forceinline__ void clear_outside(T* out, int64_t token, const int32_t* starts, int64_t n, int64_t tokens,
+                                              int dim, int extra, int extras, float* lse) {
+    if (starts == nullptr) return;
+    const int64_t before = min(max((int64_t)starts[0], (int64_t)0), tokens);
+    const int64_t after = min(max((int64_t)starts[n], before), tokens);
+    for (int64_t i = extra; i < before + tokens - after; i += extras) {
+        const int64_t t = i < before ? i : after + i - before;
+        for (int d = threadIdx.x; d < dim; d += kAttnThreads) out[t * token + d] = (T)0.0f;
+        if (lse != nullptr && threadIdx.x == 0) lse[t] = -__builtin_inff();
+    }
+}
+
+template <typename T, int DT>
+__global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attention_t a, int items) {
+    constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
+    __shared__ __attribute__((aligned(16))) uint8_t sK[2 * kTile];
+    __shared__ __attribute__((aligned(16))) uint8_t sV[2 * kTile];
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
+    const int head = head_of(blockIdx.x, a.q_heads, a.kv_heads), kv = head / (a.q_heads / a.kv_heads);
+    const Span w = find_span<kRows, false, true>((int)(blockIdx.x / a.q_heads), a.sequences, a.q_starts, a.k_starts,
+                                                 a.q_tokens, a.k_tokens);
+    T* const o_head = (T*)a.o + (int64_t)head * a.dim;
+    const int64_t o_token = (int64_t)a.q_heads * a.dim;
+    float* const lse_head = a.lse != nullptr ? a.lse + head * a.q_tokens : nullptr;
+    if (w.tile < 0) {
+        const int extras = items - ((int)(blockIdx.x / a.q_heads) - w.extra);
+        clear_outside(o_head, o_token, a.q_starts, a.sequences, a.q_tokens, a.dim, w.extra, extras, lse_head);
+        return;
+    }
+    const int off = w.keys - w.rows, r0 = w.tile * kRows, row = r0 + wave * 32 + (lane & 31);
+    const Sight sees = sight(a, w.keys);
+    const KeyTiles tiles(sees, r0 + off, min(r0 + kRows, w.rows) - 1 + off);
+    const int lo = r0 + wave * 32 + off, hi = min(r0 + wave * 32 + 31, w.rows - 1) + off;   // this wave's positions
+    const int last = sees.last(row + off), before = sees.before(row + off);
+
+    u32x4 q[kS];
+    load_operand<DT>(q, (const T*)a.q + (w.q0 + min(row, w.rows - 1)) * a.q_token + head * a.q_head, a.dim);
+
+    const TileLoads<DT, 4> lk(wave, a.k_token, a.dim), lv(wave, a.v_token, a.dim);
+    const T* const k_head = (const T*)a.k + w.k0 * a.k_token + kv * a.k_head;
+    const T* const v_head = (const T*)a.v + w.k0 * a.v_token + kv * a.v_head;
+    const uint32_t ldsK = lds_addr(sK), ldsV = lds_addr(sV);
+    auto issue = [&](int t, int buffer) {
+        const int64_t j = (int64_t)t * kKeys;
+        lk.issue(k_head + j * a.k_token, w.keys - (int)j, ldsK + buffer * kTile, wave, a.dim);
+        lv.issue(v_head + j * a.v_token, w.keys - (int)j, ldsV + buffer * kTile, wave, a.dim);
+    };
+
+    f32x16 o[kB];
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
+    const float c = a.scale * kLog2e;
+    float m = -__builtin_inff(), sum = 0.0f;         // reference and this lane's sum, in powers of two
+
+    if (tiles.n > 0) issue(tiles[0], 0);
+    for (int i = 0; i < tiles.n; ++i) {
+        wait_loads<0>();
+        barrier();
+        if (i + 1 < tiles.n) issue(tiles[i + 1], (i + 1) & 1);
+        const int j0 = tiles[i] * kKeys;
+        if (sees.none(lo, hi, j0, kKeys)) continue;
+        const uint8_t *tk = sK + (i & 1) * kTile, *tv = sV + (i & 1) * kTile;
+
+        f32x16 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
+#pragma unroll
+            for (int x = 0; x < kS; ++x) s[b] = product32<T>(read_along<DT>(tk, 32 * b, x), q[x], s[b]);
+        }
+        if (!sees.all(lo, hi, j0, kKeys)) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    s[b][e] = seen(j0 + 32 * b + 8 * (e / 4) + 4 * h + e % 4, last, before, sees.sinks) ? s[b][e] : -__builtin_inff();
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+        top = fmaxf(top, other_half(top)) * c;
+        if (__ballot(top > m + kSlack) != 0) {
+            const float next = fmaxf(m, top), f = exp2_fast(m - next);
+            const float scale = m == next ? 1.0f : f;
+            m = next;
+            sum *= scale;
+#pragma unroll
+            for (int b = 0; b < kB; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[b][e] *= scale;
+        }
+        const float ref = m == -__builtin_inff() ? 0.0f : m;
+        u32x4 pt[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const float u = exp2_fast(fmaf(s[x / 2][8 * (x % 2) + 2 * y], c, -ref));
+                const float v = exp2_fast(fmaf(s[x / 2][8 * (x % 2) + 2 * y + 1], c, -ref));
+                sum += u + v;
+                pt[x][y] = pack2<T>(u, v);
+            }
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int b = 0; b < kB; ++b) o[b] = product32<T>(read_across<DT>(tv, 16 * x, b), pt[x], o[b]);
+    }
+    sum += other_half(sum);
+    if (row >= w.rows) return;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    store_column<T, DT>(o_head + (w.q0 + row) * o_token, o, inv, a.dim);
+    if (a.o_rest != nullptr) {
+#pragma unroll
+        for (int b = 0; b < kB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[b][e] = o[b][e] * inv - (float)(T)(o[b][e] * inv);
+        store_column<T, DT>((T*)a.o_rest + (w.q0 + row) * o_token + (int64_t)head * a.dim, o, 1.0f, a.dim);
+    }
+    if (lse_head != nullptr && h == 0) lse_head[w.q0 + row] = sum == 0.0f ? -__builtin_inff() : m * kLn2 + logf(sum);
+}
+
+// dQ, and the rows' sums do . o, which both halves of the backward pass take.
+// As the forward kernel; P is exp(score - lse) and dS = P (dP - do . o) is rounded to
+// the inputs' type for its product.  dP and do . o often nearly cancel, so the rounding of
+// o would be the largest error of dS: the forward pass keeps what it left (with it dQ
+// and dK of 8192 tokens are 2.5e-3 from the exact ones in relative L2 norm, 1.7e-3 of
+// which their own rounding makes; without it 3.4e-3).
+template <typename T, int DT>
+__global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items) {
+    constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
+    __shared__ __attribute__((aligned(16))) uint8_t sK[2 * kTile];
+    __shared__ __attribute__((aligned(16))) uint8_t sV[2 * kTile];
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
+    const int head = head_of(blockIdx.x, a.q_heads, a.kv_heads), kv = head / (a.q_heads / a.kv_heads);
+    const Span w = find_span<kRows, false, true>((int)(blockIdx.x / a.q_heads), a.sequences, a.q_starts, a.k_starts,
+                                                 a.q_tokens, a.k_tokens);
+    if (w.tile < 0) {
+        const int extras = items - ((int)(blockIdx.x / a.q_heads) - w.extra);
+        if (g.dq != nullptr)
+            clear_outside((T*)g.dq + head * g.dq_head, g.dq_token, a.q_starts, a.sequences, a.q_tokens, a.dim, w.extra,
+                          extras, nullptr);
+        return;
+    }
+    const int off = w.keys - w.rows, r0 = w.tile * kRows, row = r0 + wave * 32 + (lane & 31);
+    const Sight sees = sight(a, w.keys);
+    const KeyTiles tiles(sees, r0 + off, min(r0 + kRows, w.rows) - 1 + off);
+    const int lo = r0 + wave * 32 + off, hi = min(r0 + wave * 32 + 31, w.rows - 1) + off;
+    const int last = sees.last(row + off), before = sees.before(row + off);
+    const int64_t at = w.q0 + min(row, w.rows - 1), dense = (at * a.q_heads + head) * a.dim;
+
+    u32x4 q[kS], d[kS];
+    load_operand<DT>(q, (const T*)a.q + at * a.q_token + head * a.q_head, a.dim);
+    load_operand<DT>(d, (const T*)g.d_o + dense, a.dim);
+    float delta = 0.0f;
+    {
+        u32x4 o[kS], rest[kS];
+        load_operand<DT>(o, (const T*)a.o + dense, a.dim);
+        load_operand<DT>(rest, (const T*)a.o_rest + dense, a.dim);
+#pragma unroll
+        for (int x = 0; x < kS; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const float2 u = unpack2<T>(o[x][y]), r = unpack2<T>(rest[x][y]), v = unpack2<T>(d[x][y]);
+                delta += (u.x + r.x) * v.x + (u.y + r.y) * v.y;
+            }
+    }
+    delta += other_half(delta);
+    if (h == 0 && row < w.rows) g.delta[head * a.q_tokens + at] = delta;
+    if (g.dq == nullptr) return;
+    // (of a row that sees nothing the reference makes every P 0)
+    const float lse = a.lse[head * a.q_tokens + at];
+    const float ref = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+
+    const TileLoads<DT, 4> lk(wave, a.k_token, a.dim), lv(wave, a.v_token, a.dim);
+    const T* const k_head = (const T*)a.k + w.k0 * a.k_token + kv * a.k_head;
+    const T* const v_head = (const T*)a.v + w.k0 * a.v_token + kv * a.v_head;
+    const uint32_t ldsK = lds_addr(sK), ldsV = lds_addr(sV);
+    auto issue = [&](int t, int buffer) {
+        const int64_t j = (int64_t)t * kKeys;
+        lk.issue(k_head + j * a.k_token, w.keys - (int)j, ldsK + buffer * kTile, wave, a.dim);
+        lv.issue(v_head + j * a.v_token, w.keys - (int)j, ldsV + buffer * kTile, wave, a.dim);
+    };
+    f32x16 dq[kB];
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dq[b][i] = 0.0f;
+    const float c = a.scale * kLog2e;
+
+    if (tiles.n > 0) issue(tiles[0], 0);
+    for (int i = 0; i < tiles.n; ++i) {
+        wait_loads<0>();
+        barrier();
+        if (i + 1 < tiles.n) issue(tiles[i + 1], (i + 1) & 1);
+        const int j0 = tiles[i] * kKeys;
+        if (sees.none(lo, hi, j0, kKeys)) continue;
+        const uint8_t *tk = sK + (i & 1) * kTile, *tv = sV + (i & 1) * kTile;
+        const bool all = sees.all(lo, hi, j0, kKeys);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            f32x16 s, t;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = t[e] = 0.0f;
+#pragma unroll
+            for (int x = 0; x < kS; ++x) {
+                s = product32<T>(read_along<DT>(tk, 32 * b, x), q[x], s);
+                t = product32<T>(read_along<DT>(tv, 32 * b, x), d[x], t);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = exp2_fast(fmaf(s[e], c, -ref)) * (t[e] - delta);
+            if (!all) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    s[e] = seen(j0 + 32 * b + 8 * (e / 4) + 4 * h + e % 4, last, before, sees.sinks) ? s[e] : 0.0f;
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                u32x4 ds;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) ds[y] = pack2<T>(s[8 * x + 2 * y], s[8 * x + 2 * y + 1]);
+#pragma unroll
+                for (int y = 0; y < kB; ++y) dq[y] = product32<T>(read_across<DT>(tk, 32 * b + 16 * x, y), ds, dq[y]);
+            }
+        }
+    }
+    if (row < w.rows) store_column<T, DT>((T*)g.dq + at * g.dq_token + head * g.dq_head, dq, a.scale, a.dim);
+}
+
+// dK and dV: a workgroup takes 128 keys of a key-value head, 32 a wave, and walks
+// through the queries that see them, 64 at a time, of each query head that shares
+// it in turn: the sum over those heads is made here, in a fixed order.
+template <typename T, int DT>
+__global__ __launch_bounds__(kAttnThreads, 1) void attention_dkv_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items) {
+    constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
+    __shared__ __attribute__((aligned(16))) uint8_t sQ[2 * kTile];
+    __shared__ __attribute__((aligned(16))) uint8_t sD[2 * kTile];
+    __shared__ __attribute__((aligned(16))) float sL[2 * 64], sS[2 * 64];
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
+    const int kv = blockIdx.x % a.kv_heads, group = a.q_heads / a.kv_heads;
+    const Span w = find_span<kRows, true, false>((int)(blockIdx.x / a.kv_heads), a.sequences, a.q_starts, a.k_starts,
+                                                 a.q_tokens, a.k_tokens);
+    T* const dk_head = (T*)g.dk + kv * g.dk_head;
+    T* const dv_head = (T*)g.dv + kv * g.dv_head;
+    if (w.tile < 0) {
+        const int extras = items - ((int)(blockIdx.x / a.kv_heads) - w.extra);
+        clear_outside(dk_head, g.dk_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+        clear_outside(dv_head, g.dv_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+        return;
+    }
+    const int off = w.keys - w.rows, c0 = w.tile * kRows, key = c0 + wave * 32 + (lane & 31);
+    const Sight sees = sight(a, w.keys);
+    const int wlo = c0 + wave * 32, whi = min(wlo + 31, w.keys - 1);      // this wave's keys
+    const int64_t at = w.k0 + min(key, w.keys - 1);
+
+    // rows from .. to of each head see some of the workgroup's keys
+    const int end = min(c0 + kRows, w.keys) - 1;
+    int from = 0, to = w.rows;
+    if (sees.causal) {
+        from = max(0, c0 - off);
+        if (sees.window != 0 && c0 >= sees.sinks) to = (int)min((int64_t)to, (int64_t)end + sees.window - off);
+    }
+    from = from / 64;
+    const int per = max(0, (to + 63) / 64 - from), n = per * group;
+
+    u32x4 k[kS], v[kS];
+    load_operand<DT>(k, (const T*)a.k + at * a.k_token + kv * a.k_head, a.dim);
+    load_operand<DT>(v, (const T*)a.v + at * a.v_token + kv * a.v_head, a.dim);
+
+    const int64_t o_token = (int64_t)a.q_heads * a.dim;
+    const TileLoads<DT, 4> lq(wave, a.q_token, a.dim), ld(wave, o_token, a.dim);
+    const uint32_t ldsQ = lds_addr(sQ), ldsD = lds_addr(sD), ldsL = lds_addr(sL), ldsS = lds_addr(sS);
+    auto issue = [&](int i, int buffer) {
+        const int head = kv * group + i / per, r = (from + i % per) * 64, rows = w.rows - r;
+        const int64_t first = w.q0 + r;
+        lq.issue((const T*)a.q + first * a.q_token + head * a.q_head, rows, ldsQ + buffer * kTile, wave, a.dim);
+        ld.issue((const T*)g.d_o + first * o_token + head * a.dim, rows, ldsD + buffer * kTile, wave, a.dim);
+        const int64_t one = head * a.q_tokens + first + min(lane, rows - 1);
+        if (wave == 0) load_4(a.lse + one, ldsL + buffer * 256);
+        if (wave == 1) load_4(g.delta + one, ldsS + buffer * 256);
+    };
+    f32x16 dk[kB], dv[kB];
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dk[b][i] = dv[b][i] = 0.0f;
+    const float c = a.scale * kLog2e;
+
+    if (n > 0) issue(0, 0);
+    for (int i = 0; i < n; ++i) {
+        wait_loads<0>();
+        barrier();
+        if (i + 1 < n) issue(i + 1, (i + 1) & 1);
+        const uint8_t *tq = sQ + (i & 1) * kTile, *td = sD + (i & 1) * kTile;
+        const float *tl = sL + (i & 1) * 64, *ts = sS + (i & 1) * 64;
+        const int r0 = (from + i % per) * 64;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int rb = r0 + 32 * b;
+            const int plo = rb + off, phi = min(rb + 31, w.rows - 1) + off;
+            if (rb >= w.rows || sees.none(plo, phi, wlo, whi - wlo + 1)) continue;
+            const bool all = rb + 32 <= w.rows && sees.all(plo, phi, wlo, 32);
+            f32x16 s, t;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = t[e] = 0.0f;
+#pragma unroll
+            for (int x = 0; x < kS; ++x) {
+                s = product32<T>(read_along<DT>(tq, 32 * b, x), k[x], s);
+                t = product32<T>(read_along<DT>(td, 32 * b, x), v[x], t);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f32x4 lse = *(const f32x4*)(tl + 32 * b + 8 * e + 4 * h);
+                const f32x4 delta = *(const f32x4*)(ts + 32 * b + 8 * e + 4 * h);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const float ref = lse[y] == -__builtin_inff() ? __builtin_inff() : lse[y] * kLog2e;
+                    s[4 * e + y] = exp2_fast(fmaf(s[4 * e + y], c, -ref));
+                    t[4 * e + y] = s[4 * e + y] * (t[4 * e + y] - delta[y]);
+                }
+            }
+            if (!all) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int r = rb + 8 * (e / 4) + 4 * h + e % 4;
+                    const bool ok = (r < w.rows) & seen(key, sees.last(r + off), sees.before(r + off), sees.sinks);
+                    s[e] = ok ? s[e] : 0.0f;
+                    t[e] = ok ? t[e] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                u32x4 pt, ds;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    pt[y] = pack2<T>(s[8 * x + 2 * y], s[8 * x + 2 * y + 1]);
+                    ds[y] = pack2<T>(t[8 * x + 2 * y], t[8 * x + 2 * y + 1]);
+                }
+#pragma unroll
+                for (int y = 0; y < kB; ++y) {
+                    dv[y] = product32<T>(read_across<DT>(td, 32 * b + 16 * x, y), pt, dv[y]);
+                    dk[y] = product32<T>(read_across<DT>(tq, 32 * b + 16 * x, y), ds, dk[y]);
+                }
+            }
+        }
+    }
+    if (key >= w.keys) return;
+    store_column<T, DT>(dk_head + at * g.dk_token, dk, a.scale, a.dim);
+    store_column<T, DT>(dv_head + at * g.dv_token, dv, 1.0f, a.dim);
+}
+
+// Calls f(null pointer of the type, the padded head size).
+template <typename F>
+hipError_t with_head(DType type, int dim, F&& f) {
+    auto sized = [&](auto* t) {
+        return dim <= 64 ? f(t, std::integral_constant<int, 64>{}) : f(t, std::integral_constant<int, 128>{});
+    };
+    return type == DType::BF16 ? sized((bf16*)nullptr) : sized((f16*)nullptr);
+}
+
+}  // namespace
+
+// (of ragged ones one more, for rows of none)
+int64_t attention_items(int64_t tokens, int64_t sequences, bool ragged) {
+    return ragged ? tokens / kRows + sequences + 1 : sequences * ((tokens / sequences + kRows - 1) / kRows);
+}
+
+hipError_t launch_attention(const ue5m3_attention_t& a, hipStream_t s) {
+    const int64_t items = attention_items(a.q_tokens, a.sequences, a.q_starts != nullptr);
+    return with_head((DType)a.type, a.dim, [&](auto* t, auto d) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        hipLaunchKernelGGL((attention_kernel<T, decltype(d)::value>), dim3((unsigned)(items * a.q_heads)), dim3(kAttnThreads),
+                           0, s, a, (int)items);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_attention_grad(const ue5m3_attention_t& a, const ue5m3_attention_grad_t& g, hipStream_t s) {
+    const int64_t rows = attention_items(a.q_tokens, a.sequences, a.q_starts != nullptr);
+    const int64_t keys = attention_items(a.k_tokens, a.sequences, a.k_starts != nullptr);
+    return with_head((DType)a.type, a.dim, [&](auto* t, auto d) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        constexpr int DT = decltype(d)::value;
+        hipError_t e = hipSuccess;
+        if (a.q_tokens > 0) {
+            hipLaunchKernelGGL((attention_dq_kernel<T, DT>), dim3((unsigned)(rows * a.q_heads)), dim3(kAttnThreads), 0, s, a,
+                               g, (int)rows);
+            e = hipGetLastError();
+        }
+        if (e == hipSuccess && g.dk != nullptr && a.k_tokens > 0) {
+            hipLaunchKernelGGL((attention_dkv_kernel<T, DT>), dim3((unsigned)(keys * a.kv_heads)), dim3(kAttnThreads), 0, s,
+                               a, g, (int)keys);
+            e = hipGetLastError();
+        }
+        return e;
+    });
+}
+
+}  // namespace ue5m3

@@ -1,0 +1,244 @@
+"""Norms of queries and keys for each head and their rotation by position, in
+one pass over both: with gradients, and in a serving form that writes keys and
+values into the pages of a cache.
+
+Either part may be left out (``eps=None``: no norm; ``freqs=None``: no rotation).
+Frequencies are a tensor of the caller's, so that any scaling for long contexts
+is his; ``rotary_frequencies`` makes the common ones.
+"""
+
+import math
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import PagesC, RopeC, _check, _numel, _ptr, _stream, load_library
+from .operators import _TYPES, recorded
+
+
+def rotary_frequencies(dim, base=10000.0, factor=1.0, kind="linear", original=None, low=1.0, high=32.0, device="cuda"):
+    """(freqs, amplitude) for ``qk_norm_rope``: fp32 [dim / 2], base^(-2 i / dim)
+    scaled for contexts ``factor`` times as long:
+
+      linear   all divided by ``factor``
+      base     the base raised, by factor^(dim / (dim - 2)): the last frequency is
+               divided by ``factor``, the first stays
+      parts    divided by ``factor`` where ``original`` positions (the context
+               trained on) are fewer than ``low`` turns, kept where they are more
+               than ``high``, in between in proportion; the amplitude is
+               0.1 ln(factor) + 1
+    """
+    dim = int(dim)
+    if dim < 2 or dim % 2 or not base > 1.0 or not factor >= 1.0:
+        raise ValueError("dim must be even and positive, base above 1, factor at least 1")
+    i = torch.arange(0, dim, 2, dtype=torch.float64)
+    amplitude = 1.0
+    if kind == "base":
+        if dim == 2 and factor != 1.0:
+            raise ValueError("one pair has no base to raise")
+        f = (base * factor ** (dim / max(dim - 2, 1))) ** (-i / dim)
+    else:
+        f = base ** (-i / dim)
+        if kind == "linear":
+            f = f / factor
+        elif kind == "parts":
+            if original is None or not 0 < low < high:
+                raise ValueError("parts needs the original context and 0 < low < high")
+            turns = original * f / (2 * math.pi)
+            keep = ((turns - low) / (high - low)).clamp(0.0, 1.0)
+            f = f * (keep + (1.0 - keep) / factor)
+            amplitude = 0.1 * math.log(factor) + 1.0
+        else:
+            raise ValueError("kind must be linear, base or parts")
+    return f.float().to(device), amplitude
+
+
+def _on_device(t, name):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA/HIP tensor")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, not on the device of the call")
+    return t
+
+
+def head_rows(t, name, dtypes=_TYPES, dense=False):
+    """``t`` [..., heads, dim] as (tensor, tokens, token stride, head stride): itself
+    where its strides allow, with the elements of a head together, else a copy.
+    ``dense``: as the attention kernels take it (heads apart, 16-byte aligned)."""
+    _on_device(t, name)
+    if t.dtype not in dtypes or t.dim() < 3:
+        raise ValueError(f"{name} must be [..., tokens, heads, dim] of " + ", ".join(str(d) for d in dtypes))
+    shape, stride = t.shape, t.stride()
+    ok = stride[-1] == 1 or shape[-1] == 1
+    token = stride[-3]
+    for d in range(t.dim() - 4, -1, -1):                 # leading dimensions as one
+        if shape[d] > 1:
+            inner = _numel(shape[d + 1:-2])
+            ok = ok and (inner <= 1 or stride[d] == token * inner)
+            if inner <= 1:
+                token = stride[d]
+    if dense:
+        tokens = _numel(shape[:-2])
+        ok = (ok and (tokens <= 1 or shape[-1] <= token < 1 << 23) and (shape[-2] <= 1 or stride[-2] >= shape[-1])
+              and token % 8 == 0 and stride[-2] % 8 == 0 and t.data_ptr() % 16 == 0)
+    if not ok:
+        t = t.clone() if t.is_contiguous() else t.contiguous()       # (a contiguous one is not aligned)
+        token, stride = shape[-2] * shape[-1], t.stride()
+    return t, _numel(shape[:-2]), token, stride[-2]
+
+
+def _vector(t, name, dtypes, n):
+    if t is None:
+        return None
+    _on_device(t, name)
+    if t.dtype not in dtypes or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous vector of {n} of " + ", ".join(str(d) for d in dtypes))
+    return t
+
+
+def _arguments(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude):
+    """A RopeC of all but the outputs, and the tensors that it points to."""
+    qr, tokens, q_token, q_head = head_rows(q, "q") if q is not None else (None, None, 0, 0)
+    kr, k_tokens, k_token, k_head = head_rows(k, "k")
+    lead, dim = k.shape[:-2], k.shape[-1]
+    if q is not None and (q.shape[:-2] != lead or q.shape[-1] != dim or q.dtype != k.dtype):
+        raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} must have the same tokens, head size and type")
+    if not 1 <= dim <= 256:
+        raise ValueError("heads have 1 to 256 elements")
+    norm = eps is not None
+    if not norm and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights belong to the norm: pass eps")
+    wt = next((w.dtype for w in (q_weight, k_weight) if w is not None), k.dtype)
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        _vector(w, name, (wt,) if wt in (k.dtype, torch.float32) else (k.dtype, torch.float32), dim)
+    pairs = 0
+    if freqs is not None:
+        pairs = freqs.numel()
+        _vector(freqs, "freqs", (torch.float32,), pairs)
+        if freqs.requires_grad:
+            raise ValueError("freqs have no gradient")
+        if not 1 <= pairs <= dim // 2:
+            raise ValueError(f"{pairs} frequencies for heads of {dim}")
+        if positions is not None:
+            _on_device(positions, "positions")
+            if positions.dtype not in (torch.int64, torch.int32):
+                raise ValueError("positions must be integers")
+            positions = positions.to(torch.int64).expand(lead).contiguous()
+    else:
+        positions = None
+    args = RopeC(k_tokens, q.shape[-2] if q is not None else 0, k.shape[-2], dim, pairs, _TYPES[k.dtype], _TYPES[wt],
+                 int(norm), int(bool(interleaved)), float(eps) if norm else 0.0, float(amplitude), _ptr(qr), _ptr(kr),
+                 q_token, q_head, k_token, k_head, _ptr(q_weight), _ptr(k_weight), _ptr(positions), max(int(lead[-1]), 1),
+                 _ptr(freqs))
+    return args, (qr, kr, positions)
+
+
+def _dense(args, q_out, k_out):
+    dim = args.dim
+    args.q_out, args.q_out_token, args.q_out_head = _ptr(q_out), args.q_heads * dim, dim
+    args.k_out, args.k_out_token, args.k_out_head = _ptr(k_out), args.kv_heads * dim, dim
+
+
+def _forward(q, k, *rest):
+    args, kept = _arguments(q, k, *rest)
+    q_out, k_out = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    _dense(args, q_out, k_out)
+    _check(load_library().ue5m3_qk_norm_rope(args, _stream()), "ue5m3_qk_norm_rope")
+    return q_out, k_out, kept
+
+
+class _RopeFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude):
+        q_out, k_out, (qr, kr, positions) = _forward(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude)
+        norm = eps is not None
+        ctx.save_for_backward(qr if norm else None, kr if norm else None, q_weight, k_weight, positions, freqs)
+        ctx.rest, ctx.shapes = (eps, interleaved, amplitude), (q.shape, k.shape)
+        ctx.set_materialize_grads(False)
+        return q_out, k_out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gq, gk):
+        q, k, q_weight, k_weight, positions, freqs = ctx.saved_tensors
+        if gq is None and gk is None:
+            return (None,) * 9
+        like = gq if gq is not None else gk
+        gq, gk = (torch.zeros(s, dtype=like.dtype, device=like.device) if g is None else g.contiguous()
+                  for g, s in zip((gq, gk), ctx.shapes))
+        # (without the norm the inputs do not matter: the gradients stand in for them)
+        args, kept = _arguments(gq if q is None else q, gk if k is None else k, q_weight, k_weight, positions, freqs, *ctx.rest)
+        need_q, need_k, need_qw, need_kw = ctx.needs_input_grad[:4]
+        new = lambda t, need: torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None  # noqa: E731
+        dq, dk = new(gq, need_q), new(gk, need_k)
+        dqw, dkw = new(q_weight, need_qw and q_weight is not None), new(k_weight, need_kw and k_weight is not None)
+        _dense(args, dq, dk)
+        lib, scratch = load_library(), None
+        if dqw is not None or dkw is not None:
+            n = lib.ue5m3_qk_norm_rope_grad_scratch(args.tokens, args.q_heads + args.kv_heads, args.dim)
+            scratch = torch.empty(n, dtype=torch.uint8, device=like.device)
+        _check(lib.ue5m3_qk_norm_rope_grad(args, gq.data_ptr(), gk.data_ptr(), _ptr(dqw), _ptr(dkw), _ptr(scratch), _stream()),
+               "ue5m3_qk_norm_rope_grad")
+        return dq, dk, dqw, dkw, None, None, None, None, None
+
+
+def qk_norm_rope(q, k, q_weight=None, k_weight=None, positions=None, freqs=None, eps=1e-6, interleaved=False,
+                 amplitude=1.0):
+    """Queries ``q`` [..., L, heads, dim] and keys ``k`` [..., L, kv_heads, dim] (bf16,
+    fp16 or fp32; strided views of one projection's output are fine) normed over each
+    head, times ``q_weight`` and ``k_weight`` [dim] (of their type or fp32, or None), and
+    rotated by position, with gradients (see ue5m3_qk_norm_rope).
+
+    ``freqs``: fp32, one for each rotated pair: the first 2 len(freqs) elements of a
+    head turn, in halves (i with i + len(freqs)) or, ``interleaved``, neighbours
+    together.  ``positions``: integers [..., L], broadcast over leading dimensions
+    (None: 0 .. L - 1 in each).  The weights' gradients are summed in fp32 in a fixed
+    order.  Returns new dense tensors (q, k)."""
+    if recorded(q, k, q_weight, k_weight):
+        return _RopeFn.apply(q, k, q_weight, k_weight, positions, freqs, eps, bool(interleaved), float(amplitude))
+    return _forward(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude)[:2]
+
+
+def cache_arguments(k_cache, v_cache, multiple=1):
+    """PagesC of the keys and values [pages, page_size, kv_heads, dim] of one layer."""
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        _on_device(t, name)
+        if t.dim() != 4 or t.stride(3) != 1 and t.shape[3] > 1:
+            raise ValueError(f"{name} must be [pages, page_size, kv_heads, dim], a head's elements together")
+    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.dtype != v_cache.dtype:
+        raise ValueError("k_cache and v_cache must have one shape, type and strides")
+    pages, size, _, _ = k_cache.shape
+    if size < 1 or size & (size - 1):
+        raise ValueError("pages hold a power of two of tokens")
+    page, token, head = k_cache.stride()[:3]
+    if any(s % multiple for s in (page, token, head)):
+        raise ValueError(f"the cache's strides must be multiples of {multiple} elements")
+    return PagesC(k_cache.data_ptr(), v_cache.data_ptr(), pages, size, page, token, head)
+
+
+def qk_norm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None, k_weight=None, positions=None, freqs=None,
+                        eps=1e-6, interleaved=False, amplitude=1.0):
+    """The serving form of ``qk_norm_rope``: returns the queries, and writes the keys,
+    normed and rotated, and the values ``v`` into a cache (``k_cache``, ``v_cache``
+    [pages, page_size, kv_heads, dim], any strides with a head's elements together), token
+    t at ``slots``[t] (int64) = page * page_size + place (see
+    ue5m3_qk_norm_rope_append).  A slot below 0 or past the cache writes nothing.
+    ``q`` may be None (keys that are ready: with eps=None and no freqs they are
+    copied); then None is returned."""
+    if recorded(q, k, v, q_weight, k_weight):
+        raise RuntimeError("qk_norm_rope_append has no gradients: call it under torch.no_grad()")
+    args, kept = _arguments(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude)
+    vr, tokens, v_token, v_head = head_rows(v, "v")
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError(f"v {tuple(v.shape)} must have the shape and type of k {tuple(k.shape)}")
+    cache = cache_arguments(k_cache, v_cache)
+    if k_cache.shape[2:] != k.shape[-2:] or k_cache.dtype != k.dtype:
+        raise ValueError(f"a cache of {tuple(k_cache.shape)} {k_cache.dtype} does not take keys of {tuple(k.shape)} {k.dtype}")
+    _on_device(slots, "slots")
+    if slots.dtype != torch.int64 or slots.numel() != tokens or not slots.is_contiguous():
+        raise ValueError(f"slots must be {tokens} contiguous int64 numbers")
+    q_out = None if q is None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _dense(args, q_out, None)
+    _check(load_library().ue5m3_qk_norm_rope_append(args, vr.data_ptr(), v_token, v_head, cache, slots.data_ptr(), _stream()),
+           "ue5m3_qk_norm_rope_append")
+    return q_out
