@@ -625,7 +625,7 @@ ue5m3_status_t ue5m3_linear_fp8(const void* x_bf16, int64_t T, int64_t K, int64_
  * the call returns (zero what a call does not use).  Strides are in elements,
  * the elements of a head lie together, and in every tensor heads do not
  * overlap.  These calls use no library workspace: where one needs scratch
- * memory the caller passes it (4-byte aligned, any contents), so none of them
+ * memory the caller passes it (16-byte aligned, any contents), so none of them
  * needs an earlier call before a capture, and graphs share no memory that
  * their callers do not.
  * ------------------------------------------------------------------------

@@ -122,7 +122,7 @@ ue5m3_status_t ue5m3_qk_norm_rope_grad(const ue5m3_rope_t* args, const void* dq_
     const bool sums = dq_weight != nullptr || dk_weight != nullptr;
     if (sums && !args->norm) return UE5M3_EINVAL;
     if (!aligned(dq_weight, size_of(args->weight_type)) || !aligned(dk_weight, size_of(args->weight_type)) ||
-        !aligned(scratch, 4))
+        !aligned(scratch, 16))
         return UE5M3_EALIGN;
     if (args->tokens > 0) {
         // (without the norm q and k are not read)
@@ -224,7 +224,7 @@ ue5m3_status_t ue5m3_paged_attention(const ue5m3_paged_attention_t* args, void* 
         (a.width > 0 && (a.table == nullptr || a.cache.k == nullptr || a.cache.v == nullptr)))
         return UE5M3_EINVAL;
     if (!aligned(a.q, 16) || !aligned(a.o, 16) || !aligned(a.cache.k, 16) || !aligned(a.cache.v, 16) ||
-        !aligned(a.table, 4) || !aligned(a.lengths, 4) || !aligned(scratch, 4) || (a.q_token | a.q_head) % 8 != 0)
+        !aligned(a.table, 4) || !aligned(a.lengths, 4) || !aligned(scratch, 16) || (a.q_token | a.q_head) % 8 != 0)
         return UE5M3_EALIGN;
     return status(ue5m3::launch_paged_attention(a, (float*)scratch, stream));
 }

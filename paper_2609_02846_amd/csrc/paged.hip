@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kWaves = 4, kTileKeys = 32, kCols = 16;
 constexpr int kLeastKeys = 256;                      // of a part: two tiles a wave
+constexpr int kMaxParts = 128, kMaxHead = 128;
 
 // Chunk c of a row of the values' tile lies at c ^ place: reads across rows take 32
 // bytes of 16 of them.
@@ -241,23 +242,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(ue5m3_p
     }
 }
 
-// The parts of a head's output joined: a workgroup for each, a thread an element.
+// The parts of a head's output joined: a workgroup for each, its parts in eight
+// groups (part mod 8) of 32 threads, four elements a thread; then the groups, in a
+// fixed order.
+constexpr int kJoinGroups = 8, kJoinThreads = 256;
+
 template <typename T>
-__global__ __launch_bounds__(128) void paged_join_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
-                                                         int parts, int dim, T* __restrict__ out) {
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const float* __restrict__ part_o,
+                                                                  const float* __restrict__ part_ml, int parts, int dim,
+                                                                  T* __restrict__ out) {
+    __shared__ float so[kJoinGroups][kMaxHead], sl[kJoinGroups], sm[kMaxParts];
     const int64_t at = blockIdx.x;
     const float* ml = part_ml + at * parts * 2;
+    const int group = threadIdx.x >> 5, d = 4 * (threadIdx.x & 31);
+    if ((int)threadIdx.x < parts) sm[threadIdx.x] = ml[2 * threadIdx.x];
+    __syncthreads();
     float top = -__builtin_inff();
-    for (int p = 0; p < parts; ++p) top = fmaxf(top, ml[2 * p]);
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, sm[p]);
     const float ref = top == -__builtin_inff() ? 0.0f : top;
-    const int d = threadIdx.x;
-    float v = 0.0f, l = 0.0f;
-    for (int p = 0; p < parts; ++p) {
-        const float f = exp2_fast(ml[2 * p] - ref);
+    f32x4 v = {0, 0, 0, 0};
+    float l = 0.0f;
+#pragma unroll 4
+    for (int p = group; p < parts; p += kJoinGroups) {
+        const float f = exp2_fast(sm[p] - ref);
         l += ml[2 * p + 1] * f;
-        if (d < dim) v += part_o[(at * parts + p) * dim + d] * f;
+        if (d < dim) v += *(const f32x4*)(part_o + (at * parts + p) * dim + d) * f;
     }
-    if (d < dim) out[at * dim + d] = (T)(l == 0.0f ? 0.0f : v / l);
+    if (d < dim) *(f32x4*)(&so[group][d]) = v;
+    if (d == 0) sl[group] = l;
+    __syncthreads();
+    const int e = threadIdx.x;
+    if (e >= dim) return;
+    float o = 0.0f, sum = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kJoinGroups; ++g) o += so[g][e], sum += sl[g];
+    out[at * dim + e] = (T)(sum == 0.0f ? 0.0f : o / sum);
 }
 
 }  // namespace
@@ -266,7 +285,7 @@ int paged_parts(int64_t rows, int q_heads, int kv_heads, int64_t capacity, int64
     const int group = q_heads / kv_heads;
     const int64_t work = rows * kv_heads * ((group + kCols - 1) / kCols);
     const int64_t keys = window != 0 ? std::min(capacity, std::min(window, capacity) + std::min(sinks, capacity)) : capacity;
-    const int64_t most = std::min<int64_t>((keys + kLeastKeys - 1) / kLeastKeys, 128);
+    const int64_t most = std::min<int64_t>((keys + kLeastKeys - 1) / kLeastKeys, kMaxParts);
     return (int)std::max<int64_t>(1, std::min(most, 2048 / std::max<int64_t>(work, 1)));
 }
 
@@ -287,7 +306,7 @@ hipError_t launch_paged_attention(const ue5m3_paged_attention_t& a, float* scrat
             hipLaunchKernelGGL((paged_attention_kernel<T, 128>), grid, threads, 0, s, a, parts, blocks, scratch, part_ml);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && parts > 1) {
-            hipLaunchKernelGGL((paged_join_kernel<T>), dim3((unsigned)(a.rows * a.q_heads)), dim3(128), 0, s, scratch,
+            hipLaunchKernelGGL((paged_join_kernel<T>), dim3((unsigned)(a.rows * a.q_heads)), dim3(kJoinThreads), 0, s, scratch,
                                part_ml, parts, a.dim, (T*)a.o);
             e = hipGetLastError();
         }
