@@ -766,16 +766,17 @@ ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, hipStream_t stream
  * delta = sum(d_o (o + o_rest)) of each row, dS = P (d_o . v - delta), dq = scale dS k,
  * dk = scale dS^T q, dv = P^T d_o, the last two summed over the query heads that share
  * a key-value head, in a fixed order.  `args` as of the forward call, with its o,
- * o_rest and lse; delta [q_heads][q_tokens] is scratch that the call writes.  dq, or dk and dv
+ * o_rest and lse; `scratch` has ue5m3_attention_grad_scratch(args) bytes.  dq, or dk and dv
  * together, may be null.  16-byte alignment and strides as for q, k and v.
  */
 typedef struct {
     const void* d_o;
-    float* delta;
+    void* scratch;
     void *dq, *dk, *dv;
     int64_t dq_token, dq_head, dk_token, dk_head, dv_token, dv_head;
 } ue5m3_attention_grad_t;
 
+int64_t ue5m3_attention_grad_scratch(const ue5m3_attention_t* args);
 ue5m3_status_t ue5m3_attention_grad(const ue5m3_attention_t* args, const ue5m3_attention_grad_t* grad,
                                     hipStream_t stream);
 

@@ -102,10 +102,11 @@ class _AttentionFn(torch.autograd.Function):
         new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
         dq = new(q) if need_q else None
         dk, dv = (new(k), new(v)) if need_k or need_v else (None, None)
-        delta = torch.empty_like(lse)
+        lib = load_library()
+        scratch = torch.empty(lib.ue5m3_attention_grad_scratch(args), dtype=torch.uint8, device=lse.device)
         qs, ks, d = q.shape[-2] * q.shape[-1], k.shape[-2] * k.shape[-1], q.shape[-1]
-        grad = AttentionGradC(do.data_ptr(), delta.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), qs, d, ks, d, ks, d)
-        _check(load_library().ue5m3_attention_grad(args, grad, _stream()), "ue5m3_attention_grad")
+        grad = AttentionGradC(do.data_ptr(), scratch.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), qs, d, ks, d, ks, d)
+        _check(lib.ue5m3_attention_grad(args, grad, _stream()), "ue5m3_attention_grad")
         return dq, dk if need_k else None, dv if need_v else None, None, None, None, None, None, None
 
 

@@ -86,7 +86,7 @@ ue5m3_status_t attention_args(const ue5m3_attention_t* a) {
         return UE5M3_ESHAPE;
     const bool ragged = a->q_starts != nullptr;
     if (ue5m3::attention_items(a->q_tokens, a->sequences, ragged) > kMaxGrid / a->q_heads ||
-        ue5m3::attention_items(a->k_tokens, a->sequences, ragged) > kMaxGrid / a->kv_heads ||
+        ue5m3::attention_items(a->k_tokens, a->sequences, ragged) > kMaxGrid / 8 / a->kv_heads ||
         (a->q_tokens / 64 + 2) * (a->q_heads / a->kv_heads) > 0x7FFFFFFF)
         return UE5M3_ESHAPE;
     if (a->q_tokens > 0 && (a->q == nullptr || a->o == nullptr)) return UE5M3_EINVAL;
@@ -183,14 +183,22 @@ ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, hipStream_t stream
     return status(ue5m3::launch_attention(*args, stream));
 }
 
+int64_t ue5m3_attention_grad_scratch(const ue5m3_attention_t* args) {
+    return args == nullptr || args->q_tokens < 0 || args->k_tokens < 0 || args->q_tokens > kMaxTokens ||
+                   args->k_tokens > kMaxTokens || args->sequences < 1 || args->q_heads < 1 || args->kv_heads < 1 ||
+                   args->q_heads > kMaxHeads || args->kv_heads > kMaxHeads || args->dim < 1 || args->dim > 128
+               ? 0 : ue5m3::attention_grad_scratch(*args);
+}
+
 ue5m3_status_t ue5m3_attention_grad(const ue5m3_attention_t* args, const ue5m3_attention_grad_t* grad,
                                     hipStream_t stream) {
     const ue5m3_status_t st = attention_args(args);
     if (st != UE5M3_OK) return st;
     if (grad == nullptr || (grad->dk == nullptr) != (grad->dv == nullptr)) return UE5M3_EINVAL;
     const ue5m3_attention_grad_t& g = *grad;
-    if (args->q_tokens > 0 && (g.d_o == nullptr || g.delta == nullptr || args->lse == nullptr || args->o_rest == nullptr)) return UE5M3_EINVAL;
-    if (!aligned(g.d_o, 16) || !aligned(g.delta, 4) || !aligned(g.dq, 16) || !aligned(g.dk, 16) || !aligned(g.dv, 16) ||
+    if (ue5m3::attention_grad_scratch(*args) > 0 && g.scratch == nullptr) return UE5M3_EINVAL;
+    if (args->q_tokens > 0 && (g.d_o == nullptr || args->lse == nullptr || args->o_rest == nullptr)) return UE5M3_EINVAL;
+    if (!aligned(g.d_o, 16) || !aligned(g.scratch, 16) || !aligned(g.dq, 16) || !aligned(g.dk, 16) || !aligned(g.dv, 16) ||
         (g.dq != nullptr && (g.dq_token | g.dq_head) % 8 != 0) ||
         (g.dk != nullptr && (g.dk_token | g.dk_head | g.dv_token | g.dv_head) % 8 != 0))
         return UE5M3_EALIGN;

@@ -20,6 +20,7 @@ namespace ue5m3 {
 namespace {
 
 constexpr int kAttnThreads = 256, kRows = 128, kKeys = 64;
+constexpr int kCus = 256;                            // of the device
 
 // The reference of a row's exponentials follows its maximum only where that has
 // grown by more than 2^8: until then P is at most 2^8, which loses nothing in
@@ -137,14 +138,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
     u32x4 q[kS];
     load_operand<DT>(q, (const T*)a.q + (w.q0 + min(row, w.rows - 1)) * a.q_token + head * a.q_head, a.dim);
 
-    const TileLoads<DT, 4> lk(wave, a.k_token, a.dim), lv(wave, a.v_token, a.dim);
+    const uint32_t k_bytes = (uint32_t)a.k_token * 2, v_bytes = (uint32_t)a.v_token * 2;
+    const TileLoads<DT> lk(k_bytes, wave, lane, a.dim), lv(v_bytes, wave, lane, a.dim);
     const T* const k_head = (const T*)a.k + w.k0 * a.k_token + kv * a.k_head;
     const T* const v_head = (const T*)a.v + w.k0 * a.v_token + kv * a.v_head;
     const uint32_t ldsK = lds_addr(sK), ldsV = lds_addr(sV);
     auto issue = [&](int t, int buffer) {
         const int64_t j = (int64_t)t * kKeys;
-        lk.issue(k_head + j * a.k_token, w.keys - (int)j, ldsK + buffer * kTile, wave, a.dim);
-        lv.issue(v_head + j * a.v_token, w.keys - (int)j, ldsV + buffer * kTile, wave, a.dim);
+        lk.issue(k_head + j * a.k_token, k_bytes, w.keys - (int)j, ldsK + buffer * kTile, wave, a.dim);
+        lv.issue(v_head + j * a.v_token, v_bytes, w.keys - (int)j, ldsV + buffer * kTile, wave, a.dim);
     };
 
     f32x16 o[kB];
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
 #pragma unroll
-            for (int x = 0; x < kS; ++x) s[b] = product32<T>(read_along<DT>(tk, 32 * b, x), q[x], s[b]);
+            for (int x = 0; x < kS; ++x) s[b] = product32<T>(read_along<DT>(tk, 32 * b, x, lane), q[x], s[b]);
         }
         if (!sees.all(lo, hi, j0, kKeys)) {
 #pragma unroll
@@ -207,7 +209,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
-            for (int b = 0; b < kB; ++b) o[b] = product32<T>(read_across<DT>(tv, 16 * x, b), pt[x], o[b]);
+            for (int b = 0; b < kB; ++b) o[b] = product32<T>(read_across<DT>(tv, 16 * x, b, lane), pt[x], o[b]);
     }
     sum += other_half(sum);
     if (row >= w.rows) return;
@@ -269,20 +271,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
             }
     }
     delta += other_half(delta);
-    if (h == 0 && row < w.rows) g.delta[head * a.q_tokens + at] = delta;
-    if (g.dq == nullptr) return;
     // (of a row that sees nothing the reference makes every P 0)
     const float lse = a.lse[head * a.q_tokens + at];
     const float ref = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+    if (h == 0 && row < w.rows) {
+        ((float*)g.scratch)[head * a.q_tokens + at] = delta;
+        ((float*)g.scratch)[(a.q_heads + head) * a.q_tokens + at] = ref;
+    }
+    if (g.dq == nullptr) return;
 
-    const TileLoads<DT, 4> lk(wave, a.k_token, a.dim), lv(wave, a.v_token, a.dim);
+    const uint32_t k_bytes = (uint32_t)a.k_token * 2, v_bytes = (uint32_t)a.v_token * 2;
+    const TileLoads<DT> lk(k_bytes, wave, lane, a.dim), lv(v_bytes, wave, lane, a.dim);
     const T* const k_head = (const T*)a.k + w.k0 * a.k_token + kv * a.k_head;
     const T* const v_head = (const T*)a.v + w.k0 * a.v_token + kv * a.v_head;
     const uint32_t ldsK = lds_addr(sK), ldsV = lds_addr(sV);
     auto issue = [&](int t, int buffer) {
         const int64_t j = (int64_t)t * kKeys;
-        lk.issue(k_head + j * a.k_token, w.keys - (int)j, ldsK + buffer * kTile, wave, a.dim);
-        lv.issue(v_head + j * a.v_token, w.keys - (int)j, ldsV + buffer * kTile, wave, a.dim);
+        lk.issue(k_head + j * a.k_token, k_bytes, w.keys - (int)j, ldsK + buffer * kTile, wave, a.dim);
+        lv.issue(v_head + j * a.v_token, v_bytes, w.keys - (int)j, ldsV + buffer * kTile, wave, a.dim);
     };
     f32x16 dq[kB];
 #pragma unroll
@@ -307,8 +313,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
             for (int e = 0; e < 16; ++e) s[e] = t[e] = 0.0f;
 #pragma unroll
             for (int x = 0; x < kS; ++x) {
-                s = product32<T>(read_along<DT>(tk, 32 * b, x), q[x], s);
-                t = product32<T>(read_along<DT>(tv, 32 * b, x), d[x], t);
+                s = product32<T>(read_along<DT>(tk, 32 * b, x, lane), q[x], s);
+                t = product32<T>(read_along<DT>(tv, 32 * b, x, lane), d[x], t);
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = exp2_fast(fmaf(s[e], c, -ref)) * (t[e] - delta);
@@ -323,64 +329,126 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
 #pragma unroll
                 for (int y = 0; y < 4; ++y) ds[y] = pack2<T>(s[8 * x + 2 * y], s[8 * x + 2 * y + 1]);
 #pragma unroll
-                for (int y = 0; y < kB; ++y) dq[y] = product32<T>(read_across<DT>(tk, 32 * b + 16 * x, y), ds, dq[y]);
+                for (int y = 0; y < kB; ++y) dq[y] = product32<T>(read_across<DT>(tk, 32 * b + 16 * x, y, lane), ds, dq[y]);
             }
         }
     }
     if (row < w.rows) store_column<T, DT>((T*)g.dq + at * g.dq_token + head * g.dq_head, dq, a.scale, a.dim);
 }
 
+// Of the gradient's scratch memory: delta and the references [2][heads][tokens], then
+// the parts of dK and dV [parts][2][tokens][kv_heads][dim].
+__host__ __device__ inline int64_t dkv_floats(const ue5m3_attention_t& a) { return a.k_tokens * a.kv_heads * a.dim; }
+__host__ __device__ inline int64_t delta_floats(const ue5m3_attention_t& a) { return (2 * a.q_heads * a.q_tokens + 3) / 4 * 4; }
+__device__ __forceinline__ float* dkv_parts(const ue5m3_attention_t& a, const ue5m3_attention_grad_t& g) {
+    return (float*)g.scratch + delta_floats(a);
+}
+
 // dK and dV: a workgroup takes 128 keys of a key-value head, 32 a wave, and walks
-// through the queries that see them, 64 at a time, of each query head that shares
+// through the queries that see them, 32 at a time, of each query head that shares
 // it in turn: the sum over those heads is made here, in a fixed order.
+//
+// Scores are queries x keys here, so that P and dS are the operands of the products that
+// contract over queries.  A wave's keys stay in registers, its values in LDS: with both in
+// registers there would be room for one wave a SIMD only, and nothing to fill its waits
+// (8192 tokens 1730 us against @DKV@).
 template <typename T, int DT>
-__global__ __launch_bounds__(kAttnThreads, 1) void attention_dkv_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items) {
-    constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
+__global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items,
+                                                                       int parts) {
+    constexpr int kQ = 32, kTile = kQ * DT * 2, kB = DT / 32, kS = DT / 16;
     __shared__ __attribute__((aligned(16))) uint8_t sQ[2 * kTile];
     __shared__ __attribute__((aligned(16))) uint8_t sD[2 * kTile];
-    __shared__ __attribute__((aligned(16))) float sL[2 * 64], sS[2 * 64];
+    __shared__ __attribute__((aligned(16))) uint8_t sV[kRows * DT * 2];
+    __shared__ __attribute__((aligned(16))) float sR[2 * 64];        // delta of the tile's rows, then their references
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
     const int kv = blockIdx.x % a.kv_heads, group = a.q_heads / a.kv_heads;
-    const Span w = find_span<kRows, true, false>((int)(blockIdx.x / a.kv_heads), a.sequences, a.q_starts, a.k_starts,
-                                                 a.q_tokens, a.k_tokens);
+    const int part = blockIdx.x / a.kv_heads % parts, item = blockIdx.x / (a.kv_heads * parts);
+    const Span w = find_span<kRows, true, false>(item, a.sequences, a.q_starts, a.k_starts, a.q_tokens, a.k_tokens);
+    float* const delta = (float*)g.scratch;
+    float* const part_dk = dkv_parts(a, g) + (int64_t)part * 2 * dkv_floats(a) + (int64_t)kv * a.dim;
+    float* const part_dv = part_dk + dkv_floats(a);
     T* const dk_head = (T*)g.dk + kv * g.dk_head;
     T* const dv_head = (T*)g.dv + kv * g.dv_head;
+    const int64_t token = (int64_t)a.kv_heads * a.dim;   // of the parts
     if (w.tile < 0) {
-        const int extras = items - ((int)(blockIdx.x / a.kv_heads) - w.extra);
-        clear_outside(dk_head, g.dk_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
-        clear_outside(dv_head, g.dv_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+        const int extras = items - (item - w.extra);
+        if (parts > 1) {
+            clear_outside(part_dk, token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+            clear_outside(part_dv, token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+        } else {
+            clear_outside(dk_head, g.dk_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+            clear_outside(dv_head, g.dv_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+        }
         return;
     }
     const int off = w.keys - w.rows, c0 = w.tile * kRows, key = c0 + wave * 32 + (lane & 31);
     const Sight sees = sight(a, w.keys);
-    const int wlo = c0 + wave * 32, whi = min(wlo + 31, w.keys - 1);      // this wave's keys
     const int64_t at = w.k0 + min(key, w.keys - 1);
+    // the rows that see the lane's key
+    const int first = sees.causal ? max(key - off, 0) : 0;
+    const int last = sees.causal && sees.window != 0 && key >= sees.sinks
+                         ? (int)min((int64_t)key + sees.window - 1 - off, (int64_t)w.rows - 1) : w.rows - 1;
+    // of the wave's keys the rows that see some (from some_lo, before some_hi), and all
+    const int wlo = c0 + wave * 32, whi = wlo + 31;
+    const bool limited = sees.causal && sees.window != 0;
+    const int some_lo = sees.causal ? max(0, wlo - off) : 0, all_lo = sees.causal ? max(0, whi - off) : 0;
+    int some_hi = w.rows, all_hi = w.rows;
+    if (limited && wlo >= sees.sinks) some_hi = (int)min((int64_t)w.rows, (int64_t)min(whi, w.keys - 1) + sees.window - off);
+    if (limited && whi >= sees.sinks) all_hi = (int)min((int64_t)w.rows, (int64_t)wlo + sees.window - off);
+    if (wlo >= w.keys) some_hi = 0;
+    if (whi >= w.keys) all_hi = 0;
 
-    // rows from .. to of each head see some of the workgroup's keys
+    // tiles of each head whose rows see some of the workgroup's keys
     const int end = min(c0 + kRows, w.keys) - 1;
     int from = 0, to = w.rows;
-    if (sees.causal) {
-        from = max(0, c0 - off);
-        if (sees.window != 0 && c0 >= sees.sinks) to = (int)min((int64_t)to, (int64_t)end + sees.window - off);
+    if (sees.causal) from = max(0, c0 - off);
+    if (limited && c0 >= sees.sinks) to = (int)min((int64_t)to, (int64_t)end + sees.window - off);
+    from = from / kQ;
+    // of all heads' tiles, one after the other, this part's share
+    const int per = max(0, (to + kQ - 1) / kQ - from);
+    const int i0 = (int)((int64_t)per * group * part / parts), n = (int)((int64_t)per * group * (part + 1) / parts) - i0;
+
+    const uint32_t ldsQ = lds_addr(sQ), ldsD = lds_addr(sD), ldsR = lds_addr(sR);
+    if (n > 0) {                                     // (the first turn waits for them)
+        const uint32_t v_bytes = (uint32_t)a.v_token * 2;
+        const TileLoads<DT> lv(v_bytes, wave, lane, a.dim);
+#pragma unroll
+        for (int i = 0; i < kRows / 64; ++i)
+            if (c0 + 64 * i < w.keys)
+                lv.issue((const T*)a.v + (w.k0 + c0 + 64 * i) * a.v_token + kv * a.v_head, v_bytes, w.keys - c0 - 64 * i,
+                         lds_addr(sV) + i * 64 * DT * 2, wave, a.dim);
     }
-    from = from / 64;
-    const int per = max(0, (to + 63) / 64 - from), n = per * group;
-
-    u32x4 k[kS], v[kS];
+    u32x4 k[kS];
     load_operand<DT>(k, (const T*)a.k + at * a.k_token + kv * a.k_head, a.dim);
-    load_operand<DT>(v, (const T*)a.v + at * a.v_token + kv * a.v_head, a.dim);
 
-    const int64_t o_token = (int64_t)a.q_heads * a.dim;
-    const TileLoads<DT, 4> lq(wave, a.q_token, a.dim), ld(wave, o_token, a.dim);
-    const uint32_t ldsQ = lds_addr(sQ), ldsD = lds_addr(sD), ldsL = lds_addr(sL), ldsS = lds_addr(sS);
-    auto issue = [&](int i, int buffer) {
-        const int head = kv * group + i / per, r = (from + i % per) * 64, rows = w.rows - r;
-        const int64_t first = w.q0 + r;
-        lq.issue((const T*)a.q + first * a.q_token + head * a.q_head, rows, ldsQ + buffer * kTile, wave, a.dim);
-        ld.issue((const T*)g.d_o + first * o_token + head * a.dim, rows, ldsD + buffer * kTile, wave, a.dim);
-        const int64_t one = head * a.q_tokens + first + min(lane, rows - 1);
-        if (wave == 0) load_4(a.lse + one, ldsL + buffer * 256);
-        if (wave == 1) load_4(g.delta + one, ldsS + buffer * 256);
+    // The tiles of a head come from its last to its first: causal workgroups then begin
+    // with the same rows and stay together, so that an XCD's L2 holds what they read (from
+    // the first on, each would begin at its own keys: @ASC@).
+    // The next loads: the rows from `next` on, at q_at, d_at and r_at.
+    const int top = (from + per - 1) * kQ;           // first row of the last tile
+    const int head = kv * group + (per > 0 ? i0 / per : 0), skip = per > 0 ? i0 % per * kQ : 0;
+    const int64_t o_token = (int64_t)a.q_heads * a.dim, row0 = w.q0 + top;
+    const uint32_t q_bytes = (uint32_t)a.q_token * 2, d_bytes = (uint32_t)o_token * 2;
+    const TileLoads<DT, kQ> lq(q_bytes, wave, lane, a.dim), ld(d_bytes, wave, lane, a.dim);
+    const T* q_last = (const T*)a.q + row0 * a.q_token + head * a.q_head;
+    const T* d_last = (const T*)g.d_o + row0 * o_token + (int64_t)head * a.dim;
+    const float* r_last = delta + head * a.q_tokens + row0 + (int64_t)h * a.q_heads * a.q_tokens + (lane & 31);
+    const T *q_at = q_last - skip * a.q_token, *d_at = d_last - skip * o_token;
+    int next = top - skip;
+    auto issue = [&](int buffer) {
+        const int rows = w.rows - next;
+        lq.issue(q_at, q_bytes, rows, ldsQ + buffer * kTile, wave, a.dim);
+        ld.issue(d_at, d_bytes, rows, ldsD + buffer * kTile, wave, a.dim);
+        if (wave == 0) load_4(r_last + (next - top) - max((lane & 31) - (rows - 1), 0), ldsR + buffer * 256);
+        next -= kQ;
+        q_at -= (int64_t)kQ * a.q_token;
+        d_at -= (int64_t)kQ * o_token;
+        if (next < from * kQ) {
+            next = top;
+            q_at = q_last += a.q_head;
+            d_at = d_last += a.dim;
+            r_last += a.q_tokens;
+        }
     };
     f32x16 dk[kB], dv[kB];
 #pragma unroll
@@ -389,67 +457,121 @@ __global__ __launch_bounds__(kAttnThreads, 1) void attention_dkv_kernel(ue5m3_at
         for (int i = 0; i < 16; ++i) dk[b][i] = dv[b][i] = 0.0f;
     const float c = a.scale * kLog2e;
 
-    if (n > 0) issue(0, 0);
-    for (int i = 0; i < n; ++i) {
+    if (n > 0) issue(0);
+    if (a.dim < DT && n > 0) {                       // values past the head's end: zeros, as nothing else clears them here
         wait_loads<0>();
         barrier();
-        if (i + 1 < n) issue(i + 1, (i + 1) & 1);
-        const uint8_t *tq = sQ + (i & 1) * kTile, *td = sD + (i & 1) * kTile;
-        const float *tl = sL + (i & 1) * 64, *ts = sS + (i & 1) * 64;
-        const int r0 = (from + i % per) * 64;
+        for (int e = lane; e < 32 * (DT / 8); e += 64)
+            if (8 * (e % (DT / 8)) >= a.dim)
+                *(u32x4*)(sV + wave * (32 * DT * 2) + place<DT>(e / (DT / 8), e % (DT / 8))) = u32x4{0, 0, 0, 0};
+    }
+    int rb = top - skip, left = n;
+    // One tile, in a buffer that is known when this is compiled, so that the addresses
+    // of all reads are a few registers and constants.
+    auto turn = [&](auto buffer) {
+        constexpr int B = decltype(buffer)::value;
+        wait_loads<0>();
+        barrier();
+        if (left > 1) issue(B ^ 1);
+        const int r0 = rb;
+        rb = rb > from * kQ ? rb - kQ : top;
+        if (r0 + kQ <= some_lo || r0 >= some_hi) return;
+        const bool all = r0 >= all_lo && r0 + kQ <= all_hi;
+        const uint8_t *tq = sQ + B * kTile, *td = sD + B * kTile, *tv = sV + wave * (32 * DT * 2);
+        const float* tr = sR + B * 64 + 4 * h;
+        f32x16 s, t;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int rb = r0 + 32 * b;
-            const int plo = rb + off, phi = min(rb + 31, w.rows - 1) + off;
-            if (rb >= w.rows || sees.none(plo, phi, wlo, whi - wlo + 1)) continue;
-            const bool all = rb + 32 <= w.rows && sees.all(plo, phi, wlo, 32);
-            f32x16 s, t;
+        for (int e = 0; e < 16; ++e) s[e] = t[e] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = t[e] = 0.0f;
+        for (int x = 0; x < kS; ++x) s = product32<T>(read_along<DT>(tq, 0, x, lane), k[x], s);
 #pragma unroll
-            for (int x = 0; x < kS; ++x) {
-                s = product32<T>(read_along<DT>(tq, 32 * b, x), k[x], s);
-                t = product32<T>(read_along<DT>(td, 32 * b, x), v[x], t);
-            }
+        for (int e = 0; e < 4; ++e) {
+            const f32x4 ref = *(const f32x4*)(tr + 32 + 8 * e);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const f32x4 lse = *(const f32x4*)(tl + 32 * b + 8 * e + 4 * h);
-                const f32x4 delta = *(const f32x4*)(ts + 32 * b + 8 * e + 4 * h);
+            for (int y = 0; y < 4; ++y) s[4 * e + y] = exp2_fast(fmaf(s[4 * e + y], c, -ref[y]));
+        }
+        const int lo = first - r0 - 4 * h, hi = last - r0 - 4 * h;
+        if (!all) {
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const float ref = lse[y] == -__builtin_inff() ? __builtin_inff() : lse[y] * kLog2e;
-                    s[4 * e + y] = exp2_fast(fmaf(s[4 * e + y], c, -ref));
-                    t[4 * e + y] = s[4 * e + y] * (t[4 * e + y] - delta[y]);
-                }
-            }
-            if (!all) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int r = rb + 8 * (e / 4) + 4 * h + e % 4;
-                    const bool ok = (r < w.rows) & seen(key, sees.last(r + off), sees.before(r + off), sees.sinks);
-                    s[e] = ok ? s[e] : 0.0f;
-                    t[e] = ok ? t[e] : 0.0f;
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                u32x4 pt, ds;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    pt[y] = pack2<T>(s[8 * x + 2 * y], s[8 * x + 2 * y + 1]);
-                    ds[y] = pack2<T>(t[8 * x + 2 * y], t[8 * x + 2 * y + 1]);
-                }
-#pragma unroll
-                for (int y = 0; y < kB; ++y) {
-                    dv[y] = product32<T>(read_across<DT>(td, 32 * b + 16 * x, y), pt, dv[y]);
-                    dk[y] = product32<T>(read_across<DT>(tq, 32 * b + 16 * x, y), ds, dk[y]);
-                }
+            for (int e = 0; e < 16; ++e) {
+                const int r = 8 * (e / 4) + e % 4;
+                s[e] = (r >= lo) & (r <= hi) ? s[e] : 0.0f;
             }
         }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            u32x4 pt;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) pt[y] = pack2<T>(s[8 * x + 2 * y], s[8 * x + 2 * y + 1]);
+#pragma unroll
+            for (int y = 0; y < kB; ++y) dv[y] = product32<T>(read_across<DT>(td, 16 * x, y, lane), pt, dv[y]);
+        }
+#pragma unroll
+        for (int x = 0; x < kS; ++x)
+            t = product32<T>(read_along<DT>(td, 0, x, lane), read_along<DT>(tv, 0, x, lane), t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f32x4 delta = *(const f32x4*)(tr + 8 * e);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) s[4 * e + y] *= t[4 * e + y] - delta[y];
+        }
+        if (!all) {                                  // (0 times what is not finite)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = 8 * (e / 4) + e % 4;
+                s[e] = (r >= lo) & (r <= hi) ? s[e] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            u32x4 ds;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) ds[y] = pack2<T>(s[8 * x + 2 * y], s[8 * x + 2 * y + 1]);
+#pragma unroll
+            for (int y = 0; y < kB; ++y) dk[y] = product32<T>(read_across<DT>(tq, 16 * x, y, lane), ds, dk[y]);
+        }
+    };
+    while (left > 0) {
+        turn(std::integral_constant<int, 0>{});
+        if (--left == 0) break;
+        turn(std::integral_constant<int, 1>{});
+        --left;
     }
     if (key >= w.keys) return;
-    store_column<T, DT>(dk_head + at * g.dk_token, dk, a.scale, a.dim);
-    store_column<T, DT>(dv_head + at * g.dv_token, dv, 1.0f, a.dim);
+    if (parts > 1) {
+#pragma unroll
+        for (int b = 0; b < kB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int d = 32 * b + 8 * e + 4 * h;
+                if (d < a.dim) {
+                    *(f32x4*)(part_dk + at * token + d) = f32x4{dk[b][4 * e], dk[b][4 * e + 1], dk[b][4 * e + 2], dk[b][4 * e + 3]};
+                    *(f32x4*)(part_dv + at * token + d) = f32x4{dv[b][4 * e], dv[b][4 * e + 1], dv[b][4 * e + 2], dv[b][4 * e + 3]};
+                }
+            }
+    } else {
+        store_column<T, DT>(dk_head + at * g.dk_token, dk, a.scale, a.dim);
+        store_column<T, DT>(dv_head + at * g.dv_token, dv, 1.0f, a.dim);
+    }
+}
+
+// dK and dV from their parts, in their order; a thread four elements of both.
+template <typename T>
+__global__ __launch_bounds__(kAttnThreads) void attention_dkv_sum_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int parts) {
+    const int64_t n = dkv_floats(a), i = ((int64_t)blockIdx.x * kAttnThreads + threadIdx.x) * 4;
+    if (i >= n) return;
+    const float* p = dkv_parts(a, g) + i;
+    f32x4 dk = {0, 0, 0, 0}, dv = {0, 0, 0, 0};
+    for (int k = 0; k < parts; ++k, p += 2 * n) {
+        dk += *(const f32x4*)p;
+        dv += *(const f32x4*)(p + n);
+    }
+    const int64_t row = i / a.dim, token = row / a.kv_heads;
+    const int d = (int)(i - row * a.dim), kv = (int)(row - token * a.kv_heads);
+    dk *= a.scale;
+    const u32x2 k2 = {pack2<T>(dk[0], dk[1]), pack2<T>(dk[2], dk[3])}, v2 = {pack2<T>(dv[0], dv[1]), pack2<T>(dv[2], dv[3])};
+    __builtin_memcpy((T*)g.dk + token * g.dk_token + kv * g.dk_head + d, &k2, 8);
+    __builtin_memcpy((T*)g.dv + token * g.dv_token + kv * g.dv_head + d, &v2, 8);
 }
 
 // Calls f(null pointer of the type, the padded head size).
@@ -478,9 +600,26 @@ hipError_t launch_attention(const ue5m3_attention_t& a, hipStream_t s) {
     });
 }
 
+// Parts that a key tile's queries are cut into.  Causal tiles differ in length, and two
+// workgroups run on a CU: with four for each CU, the longest first, all CUs end together
+// (8192 tokens, 8 key-value heads: one part 2018 us, two @P2@ with their sum).  A part has
+// 16 tiles of queries at least, by the sequences' mean length.
+int dkv_parts_of(const ue5m3_attention_t& a) {
+    if (a.q_tokens == 0 || a.k_tokens == 0) return 1;
+    const int64_t tiles = std::max<int64_t>((a.k_tokens + kRows - 1) / kRows, a.sequences), work = tiles * a.kv_heads;
+    const int64_t rows = a.q_tokens / a.sequences, turns = (rows + 31) / 32 * (a.q_heads / a.kv_heads);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({8, (4 * kCus + work - 1) / work, turns / 16}));
+}
+
+int64_t attention_grad_scratch(const ue5m3_attention_t& a) {
+    const int parts = dkv_parts_of(a);
+    return (delta_floats(a) + (parts > 1 ? 2 * parts * dkv_floats(a) : 0)) * 4;
+}
+
 hipError_t launch_attention_grad(const ue5m3_attention_t& a, const ue5m3_attention_grad_t& g, hipStream_t s) {
     const int64_t rows = attention_items(a.q_tokens, a.sequences, a.q_starts != nullptr);
     const int64_t keys = attention_items(a.k_tokens, a.sequences, a.k_starts != nullptr);
+    const int parts = dkv_parts_of(a);
     return with_head((DType)a.type, a.dim, [&](auto* t, auto d) {
         using T = std::remove_pointer_t<decltype(t)>;
         constexpr int DT = decltype(d)::value;
@@ -490,12 +629,15 @@ hipError_t launch_attention_grad(const ue5m3_attention_t& a, const ue5m3_attenti
                                g, (int)rows);
             e = hipGetLastError();
         }
-        if (e == hipSuccess && g.dk != nullptr && a.k_tokens > 0) {
-            hipLaunchKernelGGL((attention_dkv_kernel<T, DT>), dim3((unsigned)(keys * a.kv_heads)), dim3(kAttnThreads), 0, s,
-                               a, g, (int)keys);
-            e = hipGetLastError();
-        }
-        return e;
+        if (e != hipSuccess || g.dk == nullptr || a.k_tokens == 0) return e;
+        hipLaunchKernelGGL((attention_dkv_kernel<T, DT>), dim3((unsigned)(keys * parts * a.kv_heads)), dim3(kAttnThreads), 0,
+                           s, a, g, (int)keys, parts);
+        e = hipGetLastError();
+        if (e != hipSuccess || parts == 1) return e;
+        const int64_t threads = (dkv_floats(a) + 3) / 4;
+        hipLaunchKernelGGL((attention_dkv_sum_kernel<T>), dim3((unsigned)((threads + kAttnThreads - 1) / kAttnThreads)),
+                           dim3(kAttnThreads), 0, s, a, g, parts);
+        return hipGetLastError();
     });
 }
 

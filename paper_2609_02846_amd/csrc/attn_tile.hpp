@@ -86,6 +86,13 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // The value of the lane in the other half of the wave.
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
+// Number v, as a value that the compiler works out where it is used: kept over a loop, a
+// kernel's addresses would fill its registers.
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // ---- tiles in LDS ---------------------------------------------------------
 template <int DT>
 __device__ __forceinline__ int swizzle(int row) {
@@ -98,18 +105,17 @@ __device__ __forceinline__ int place(int row, int c) { return row * (2 * DT) + (
 
 // Lane l's operand of rows r0 + l % 32 (r0 a multiple of 32), elements 16 s + 8 h ..
 template <int DT>
-__device__ __forceinline__ u32x4 read_along(const uint8_t* tile, int r0, int s) {
-    const int l = threadIdx.x & 63;
-    return *(const u32x4*)(tile + r0 * (2 * DT) + place<DT>(l & 31, 2 * s + (l >> 5)));
+__device__ __forceinline__ u32x4 read_along(const uint8_t* tile, int r0, int s, int l) {
+    return *(const u32x4*)(tile + r0 * (2 * DT) + (place<DT>(l & 31, l >> 5) ^ 32 * s));
 }
 
 // Lane l's operand across 16 rows from r0 on (a multiple of 16), column 32 b + l % 32:
 // rows r0 + 4 h + {0 .. 3}, then r0 + 8 + 4 h + {0 .. 3}.  The read hands each
 // group of 16 lanes four rows of 16 columns, transposed.
 template <int DT>
-__device__ __forceinline__ u32x4 read_across(const uint8_t* tile, int r0, int b) {
+__device__ __forceinline__ u32x4 read_across(const uint8_t* tile, int r0, int b, int l) {
     typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-    const int l = threadIdx.x & 63, c = 4 * b + 2 * (l >> 4 & 1) + (l >> 1 & 1), row = 4 * (l >> 5) + (l >> 2 & 3);
+    const int c = 4 * b + 2 * (l >> 4 & 1) + (l >> 1 & 1), row = 4 * (l >> 5) + (l >> 2 & 3);
     const uint8_t* p = tile + r0 * (2 * DT) + 8 * (l & 1);
     const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + place<DT>(row, c))));
     const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + place<DT>(row + 8, c))));
@@ -148,39 +154,35 @@ __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
 }
 
-// A wave's share of the loads of a tile of 64 rows, W waves loading: NI loads of
-// RPI rows each.  Past `rows` the last row is read again: what is masked has to
-// be finite, as 0 times it is added.
-template <int DT, int W>
+// A wave's share of the loads of a tile of ROWS rows, four waves loading: kN loads of
+// kRpi rows each.  Past `rows` the last row is read again: what is masked has to
+// be finite, as 0 times it is added.  A chunk past the head's end is replaced by the
+// first one.
+template <int DT, int ROWS = 64>
 struct TileLoads {
-    static constexpr int kChunks = DT / 8, kRpi = 64 / kChunks, kN = 64 / kRpi / W;
+    static constexpr int kChunks = DT / 8, kRpi = 64 / kChunks, kN = ROWS / kRpi / 4;
     uint32_t voff[kN];                               // of a whole tile
-    uint32_t row_bytes;
 
-    __device__ __forceinline__ static int row(int wave, int n) {
-        return (wave * kN + n) * kRpi + (int)(threadIdx.x & 63) / kChunks;
+    __device__ __forceinline__ static uint32_t offset(int n, int rows, uint32_t row_bytes, int wave, int lane, int dim) {
+        const int row = (wave * kN + n) * kRpi + lane / kChunks, c = lane % kChunks ^ swizzle<DT>(row);
+        return (uint32_t)min(row, rows - 1) * row_bytes + (uint32_t)(8 * c < dim ? 16 * c : 0);
     }
-    // A chunk past the head's end is replaced by the first one.
-    __device__ __forceinline__ static uint32_t chunk(int row, int dim) {
-        const int c = (int)(threadIdx.x & 63) % kChunks ^ swizzle<DT>(row);
-        return (uint32_t)(8 * c < dim ? c : 0) * 16;
-    }
-    __device__ __forceinline__ TileLoads(int wave, int64_t token_stride, int dim) : row_bytes((uint32_t)token_stride * 2) {
+    __device__ __forceinline__ TileLoads(uint32_t row_bytes, int wave, int lane, int dim) {
 #pragma unroll
-        for (int n = 0; n < kN; ++n) voff[n] = (uint32_t)row(wave, n) * row_bytes + chunk(row(wave, n), dim);
+        for (int n = 0; n < kN; ++n) voff[n] = offset(n, ROWS, row_bytes, wave, lane, dim);
     }
     // The tile whose first row is at `first`; `rows` > 0 of its rows are there.
-    __device__ __forceinline__ void issue(const void* first, int rows, uint32_t lds, int wave, int dim) const {
-        const i32x4_t rsrc = {(int)(uint32_t)(uintptr_t)first, (int)(uint32_t)((uint64_t)(uintptr_t)first >> 32), 0x7FFFFFFF,
-                              0x00020000};
+    __device__ __forceinline__ void issue(const void* first, uint32_t row_bytes, int rows, uint32_t lds, int wave,
+                                          int dim) const {
+        const i32x4_t rsrc = buffer_rsrc(first, 0x7FFFFFFF);
         lds += (uint32_t)wave * kN * 1024;
-        if (rows >= 64) {
+        if (rows >= ROWS) {
 #pragma unroll
             for (int n = 0; n < kN; ++n) load_rows(rsrc, voff[n], lds + n * 1024);
         } else {
+            const int lane = here((int)(threadIdx.x & 63));
 #pragma unroll
-            for (int n = 0; n < kN; ++n)
-                load_rows(rsrc, (uint32_t)min(row(wave, n), rows - 1) * row_bytes + chunk(row(wave, n), dim), lds + n * 1024);
+            for (int n = 0; n < kN; ++n) load_rows(rsrc, offset(n, rows, row_bytes, wave, lane, dim), lds + n * 1024);
         }
     }
 };

@@ -137,19 +137,19 @@ def test_attention(lib):
 
 def test_attention_grad(lib):
     def call(grad=None, **kw):
-        a = dict(d_o=PTR, delta=PTR, dq=PTR, dk=PTR, dv=PTR, dq_token=256, dq_head=64, dk_token=128, dk_head=64, dv_token=128, dv_head=64)
+        a = dict(d_o=PTR, scratch=PTR, dq=PTR, dk=PTR, dv=PTR, dq_token=256, dq_head=64, dk_token=128, dk_head=64, dv_token=128, dv_head=64)
         a.update(grad or {})
         return lib.ue5m3_attention_grad(attention_args(**kw), AttentionGradC(**a), None)
     assert call() == OK and call(dict(dq=None, dk=None, dv=None)) == OK
     for kw, want in BAD_ATTENTION:
         assert call(**kw) == want, kw
     assert call(dict(dk=None)) == EINVAL and call(dict(dv=None)) == EINVAL
-    for null in ("d_o", "delta"):
+    for null in ("d_o", "scratch"):
         assert call({null: None}, q_tokens=1) == EINVAL
     assert call(q_tokens=1, lse=None) == EINVAL and call(q_tokens=1, o_rest=None) == EINVAL
     for odd in ("d_o", "dq", "dk", "dv"):
         assert call({odd: 0x100008}) == EALIGN
-    assert call(dict(delta=HALF)) == EALIGN and call(dict(dq_head=12)) == EALIGN and call(dict(dv_token=4)) == EALIGN
+    assert call(dict(scratch=HALF)) == EALIGN and call(dict(dq_head=12)) == EALIGN and call(dict(dv_token=4)) == EALIGN
     assert lib.ue5m3_attention_grad(attention_args(), None, None) == EINVAL
 
 
