@@ -33,13 +33,22 @@ struct Sight {                                       // what the rows of a seque
     // The keys j that position p sees: j <= last and (j > before or j < sinks).
     __device__ __forceinline__ int last(int p) const { return causal ? min(p, keys - 1) : keys - 1; }
     __device__ __forceinline__ int before(int p) const { return causal && window != 0 ? p - window : -1; }
-    // Whether rows at positions lo .. hi all see keys j .. j + n - 1, or none does.
-    __device__ __forceinline__ bool all(int lo, int hi, int j, int n) const {
-        return j + n <= keys && (!causal || (j + n - 1 <= lo && (window == 0 || hi - j < window || j + n <= sinks)));
+};
+
+// Which tiles of keys the rows of a wave, at positions lo .. hi, see: some of those from
+// key j on if j < some_hi and (j + kKeys > some_lo or j < sinks), all if j + kKeys <=
+// all_hi and (j >= all_lo or j + kKeys <= sinks).
+struct WaveSight {
+    int some_lo, some_hi, all_lo, all_hi, sinks;
+    __device__ __forceinline__ WaveSight(const Sight& s, int lo, int hi) : sinks(s.sinks) {
+        some_hi = s.causal ? min(hi + 1, s.keys) : s.keys;
+        all_hi = s.causal ? min(lo + 1, s.keys) : s.keys;
+        const bool limited = s.causal && s.window != 0;
+        some_lo = limited ? lo - s.window + 1 : 0;
+        all_lo = limited ? hi - s.window + 1 : 0;
     }
-    __device__ __forceinline__ bool none(int lo, int hi, int j, int n) const {
-        return j >= keys || (causal && (j > hi || (window != 0 && lo - (j + n - 1) >= window && j >= sinks)));
-    }
+    __device__ __forceinline__ bool none(int j) const { return j >= some_hi || (j + kKeys <= some_lo && j >= sinks); }
+    __device__ __forceinline__ bool all(int j) const { return j + kKeys <= all_hi && (j >= all_lo || j + kKeys <= sinks); }
 };
 
 // (selects without a branch)
@@ -132,7 +141,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
     const int off = w.keys - w.rows, r0 = w.tile * kRows, row = r0 + wave * 32 + (lane & 31);
     const Sight sees = sight(a, w.keys);
     const KeyTiles tiles(sees, r0 + off, min(r0 + kRows, w.rows) - 1 + off);
-    const int lo = r0 + wave * 32 + off, hi = min(r0 + wave * 32 + 31, w.rows - 1) + off;   // this wave's positions
+    const WaveSight mine(sees, r0 + wave * 32 + off, min(r0 + wave * 32 + 31, w.rows - 1) + off);
     const int last = sees.last(row + off), before = sees.before(row + off);
 
     u32x4 q[kS];
@@ -157,14 +166,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
     const float c = a.scale * kLog2e;
     float m = -__builtin_inff(), sum = 0.0f;         // reference and this lane's sum, in powers of two
 
-    if (tiles.n > 0) issue(tiles[0], 0);
-    for (int i = 0; i < tiles.n; ++i) {
+    // One tile, in a buffer that is known when this is compiled, so that the addresses
+    // of all reads are a few registers and constants.
+    int i = 0;
+    auto turn = [&](auto buffer) {
+        constexpr int B = decltype(buffer)::value;
         wait_loads<0>();
         barrier();
-        if (i + 1 < tiles.n) issue(tiles[i + 1], (i + 1) & 1);
         const int j0 = tiles[i] * kKeys;
-        if (sees.none(lo, hi, j0, kKeys)) continue;
-        const uint8_t *tk = sK + (i & 1) * kTile, *tv = sV + (i & 1) * kTile;
+        if (++i < tiles.n) issue(tiles[i], B ^ 1);
+        if (mine.none(j0)) return;
+        const uint8_t *tk = sK + B * kTile, *tv = sV + B * kTile;
 
         f32x16 s[2];
 #pragma unroll
@@ -174,12 +186,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
 #pragma unroll
             for (int x = 0; x < kS; ++x) s[b] = product32<T>(read_along<DT>(tk, 32 * b, x, lane), q[x], s[b]);
         }
-        if (!sees.all(lo, hi, j0, kKeys)) {
+        if (!mine.all(j0)) {
+            const int end = last - j0 - 4 * h, start = before - j0 - 4 * h, sinks = sees.sinks - j0 - 4 * h;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    s[b][e] = seen(j0 + 32 * b + 8 * (e / 4) + 4 * h + e % 4, last, before, sees.sinks) ? s[b][e] : -__builtin_inff();
+                    s[b][e] = seen(32 * b + 8 * (e / 4) + e % 4, end, start, sinks) ? s[b][e] : -__builtin_inff();
         }
         float top = s[0][0];
 #pragma unroll
@@ -196,20 +209,25 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
                 for (int e = 0; e < 16; ++e) o[b][e] *= scale;
         }
         const float ref = m == -__builtin_inff() ? 0.0f : m;
-        u32x4 pt[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < 4; ++x) {
+            u32x4 pt;
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 const float u = exp2_fast(fmaf(s[x / 2][8 * (x % 2) + 2 * y], c, -ref));
                 const float v = exp2_fast(fmaf(s[x / 2][8 * (x % 2) + 2 * y + 1], c, -ref));
                 sum += u + v;
-                pt[x][y] = pack2<T>(u, v);
+                pt[y] = pack2<T>(u, v);
             }
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int b = 0; b < kB; ++b) o[b] = product32<T>(read_across<DT>(tv, 16 * x, b, lane), pt[x], o[b]);
+            for (int b = 0; b < kB; ++b) o[b] = product32<T>(read_across<DT>(tv, 16 * x, b, lane), pt, o[b]);
+        }
+    };
+    if (tiles.n > 0) issue(tiles[0], 0);
+    while (i < tiles.n) {
+        turn(std::integral_constant<int, 0>{});
+        if (i >= tiles.n) break;
+        turn(std::integral_constant<int, 1>{});
     }
     sum += other_half(sum);
     if (row >= w.rows) return;
@@ -250,7 +268,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
     const int off = w.keys - w.rows, r0 = w.tile * kRows, row = r0 + wave * 32 + (lane & 31);
     const Sight sees = sight(a, w.keys);
     const KeyTiles tiles(sees, r0 + off, min(r0 + kRows, w.rows) - 1 + off);
-    const int lo = r0 + wave * 32 + off, hi = min(r0 + wave * 32 + 31, w.rows - 1) + off;
+    const WaveSight mine(sees, r0 + wave * 32 + off, min(r0 + wave * 32 + 31, w.rows - 1) + off);
     const int last = sees.last(row + off), before = sees.before(row + off);
     const int64_t at = w.q0 + min(row, w.rows - 1), dense = (at * a.q_heads + head) * a.dim;
 
@@ -297,15 +315,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
         for (int i = 0; i < 16; ++i) dq[b][i] = 0.0f;
     const float c = a.scale * kLog2e;
 
-    if (tiles.n > 0) issue(tiles[0], 0);
-    for (int i = 0; i < tiles.n; ++i) {
+    int i = 0;
+    auto turn = [&](auto buffer) {
+        constexpr int B = decltype(buffer)::value;
         wait_loads<0>();
         barrier();
-        if (i + 1 < tiles.n) issue(tiles[i + 1], (i + 1) & 1);
         const int j0 = tiles[i] * kKeys;
-        if (sees.none(lo, hi, j0, kKeys)) continue;
-        const uint8_t *tk = sK + (i & 1) * kTile, *tv = sV + (i & 1) * kTile;
-        const bool all = sees.all(lo, hi, j0, kKeys);
+        if (++i < tiles.n) issue(tiles[i], B ^ 1);
+        if (mine.none(j0)) return;
+        const uint8_t *tk = sK + B * kTile, *tv = sV + B * kTile;
+        const bool all = mine.all(j0);
+        const int end = last - j0 - 4 * h, start = before - j0 - 4 * h, sinks = sees.sinks - j0 - 4 * h;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             f32x16 s, t;
@@ -320,8 +340,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
             for (int e = 0; e < 16; ++e) s[e] = exp2_fast(fmaf(s[e], c, -ref)) * (t[e] - delta);
             if (!all) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    s[e] = seen(j0 + 32 * b + 8 * (e / 4) + 4 * h + e % 4, last, before, sees.sinks) ? s[e] : 0.0f;
+                for (int e = 0; e < 16; ++e) s[e] = seen(32 * b + 8 * (e / 4) + e % 4, end, start, sinks) ? s[e] : 0.0f;
             }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -332,6 +351,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
                 for (int y = 0; y < kB; ++y) dq[y] = product32<T>(read_across<DT>(tk, 32 * b + 16 * x, y, lane), ds, dq[y]);
             }
         }
+    };
+    if (tiles.n > 0) issue(tiles[0], 0);
+    while (i < tiles.n) {
+        turn(std::integral_constant<int, 0>{});
+        if (i >= tiles.n) break;
+        turn(std::integral_constant<int, 1>{});
     }
     if (row < w.rows) store_column<T, DT>((T*)g.dq + at * g.dq_token + head * g.dq_head, dq, a.scale, a.dim);
 }
