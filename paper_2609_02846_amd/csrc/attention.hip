@@ -152,13 +152,16 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
     const T* const k_head = (const T*)a.k + w.k0 * a.k_token + kv * a.k_head;
     const T* const v_head = (const T*)a.v + w.k0 * a.v_token + kv * a.v_head;
     const uint32_t ldsK = lds_addr(sK), ldsV = lds_addr(sV);
-    auto issue = [&](int t, int buffer) {
+    auto issue_k = [&](int t, int buffer) {
         const int64_t j = (int64_t)t * kKeys;
         lk.issue(k_head + j * a.k_token, k_bytes, w.keys - (int)j, ldsK + buffer * kTile, wave, a.dim);
+    };
+    auto issue_v = [&](int t, int buffer) {
+        const int64_t j = (int64_t)t * kKeys;
         lv.issue(v_head + j * a.v_token, v_bytes, w.keys - (int)j, ldsV + buffer * kTile, wave, a.dim);
     };
 
-    f32x16 o[kB];
+    f32x16 o[kB], s[2];
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
@@ -166,64 +169,104 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
     const float c = a.scale * kLog2e;
     float m = -__builtin_inff(), sum = 0.0f;         // reference and this lane's sum, in powers of two
 
-    // One tile, in a buffer that is known when this is compiled, so that the addresses
-    // of all reads are a few registers and constants.
+    // One 16 elements' step of the scores of the tile in tk.
+    auto score = [&](const uint8_t* tk, int x, f32x16 (&to)[2]) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) to[b] = product32<T>(read_along<DT>(tk, 32 * b, x, lane), q[x], to[b]);
+    };
+    auto clear = [](f32x16 (&to)[2]) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) to[b][e] = 0.0f;
+    };
+    // One tile: its scores are there, and the next one's are computed between its
+    // exponentials.  The buffer is known when this is compiled, so that the addresses of
+    // all reads are a few registers and constants.
     int i = 0;
     auto turn = [&](auto buffer) {
-        constexpr int B = decltype(buffer)::value;
+        constexpr int B = decltype(buffer)::value;   // of this tile's values, and the tile's after the next keys
         wait_loads<0>();
         barrier();
         const int j0 = tiles[i] * kKeys;
-        if (++i < tiles.n) issue(tiles[i], B ^ 1);
-        if (mine.none(j0)) return;
-        const uint8_t *tk = sK + B * kTile, *tv = sV + B * kTile;
-
-        f32x16 s[2];
+        ++i;
+        if (i + 1 < tiles.n) issue_k(tiles[i + 1], B);
+        if (i < tiles.n) issue_v(tiles[i], B ^ 1);
+        const uint8_t *tk = sK + (B ^ 1) * kTile, *tv = sV + B * kTile;
+        f32x16 ahead[2];
+        clear(ahead);
+        if (mine.none(j0)) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+            for (int x = 0; x < kS; ++x) score(tk, x, ahead);
+        } else {
+            if (!mine.all(j0)) {
+                const int end = last - j0 - 4 * h, start = before - j0 - 4 * h, sinks = sees.sinks - j0 - 4 * h;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[b][e] = 0.0f;
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int x = 0; x < kS; ++x) s[b] = product32<T>(read_along<DT>(tk, 32 * b, x, lane), q[x], s[b]);
-        }
-        if (!mine.all(j0)) {
-            const int end = last - j0 - 4 * h, start = before - j0 - 4 * h, sinks = sees.sinks - j0 - 4 * h;
+                    for (int e = 0; e < 16; ++e)
+                        s[b][e] = seen(32 * b + 8 * (e / 4) + e % 4, end, start, sinks) ? s[b][e] : -__builtin_inff();
+            }
+            float top = s[0][0];
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+            top = fmaxf(top, other_half(top)) * c;
+            if (__ballot(top > m + kSlack) != 0) {
+                const float next = fmaxf(m, top), f = exp2_fast(m - next);
+                const float scale = m == next ? 1.0f : f;
+                m = next;
+                sum *= scale;
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    s[b][e] = seen(32 * b + 8 * (e / 4) + e % 4, end, start, sinks) ? s[b][e] : -__builtin_inff();
-        }
-        float top = s[0][0];
+                for (int b = 0; b < kB; ++b)
 #pragma unroll
-        for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
-        top = fmaxf(top, other_half(top)) * c;
-        if (__ballot(top > m + kSlack) != 0) {
-            const float next = fmaxf(m, top), f = exp2_fast(m - next);
-            const float scale = m == next ? 1.0f : f;
-            m = next;
-            sum *= scale;
+                    for (int e = 0; e < 16; ++e) o[b][e] *= scale;
+            }
+            const float ref = m == -__builtin_inff() ? 0.0f : m;
+            u32x4 pt[4];
 #pragma unroll
-            for (int b = 0; b < kB; ++b)
+            for (int x = 0; x < 4; ++x) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[b][e] *= scale;
-        }
-        const float ref = m == -__builtin_inff() ? 0.0f : m;
+                for (int y = 0; y < 4; ++y) {
+                    const float u = exp2_fast(fmaf(s[x / 2][8 * (x % 2) + 2 * y], c, -ref));
+                    const float v = exp2_fast(fmaf(s[x / 2][8 * (x % 2) + 2 * y + 1], c, -ref));
+                    sum += u + v;
+                    pt[x][y] = pack2<T>(u, v);
+                }
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            u32x4 pt;
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const float u = exp2_fast(fmaf(s[x / 2][8 * (x % 2) + 2 * y], c, -ref));
-                const float v = exp2_fast(fmaf(s[x / 2][8 * (x % 2) + 2 * y + 1], c, -ref));
-                sum += u + v;
-                pt[y] = pack2<T>(u, v);
+                for (int z = 0; z < kS / 4; ++z) score(tk, x * (kS / 4) + z, ahead);
             }
 #pragma unroll
-            for (int b = 0; b < kB; ++b) o[b] = product32<T>(read_across<DT>(tv, 16 * x, b, lane), pt, o[b]);
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int b = 0; b < kB; ++b) o[b] = product32<T>(read_across<DT>(tv, 16 * x, b, lane), pt[x], o[b]);
+            // products and exponentials in turn, operands read ahead of both
+            __builtin_amdgcn_sched_group_barrier(kSgDsRead, 4, 0);
+#pragma unroll
+            for (int x = 0; x < 2 * kS; ++x) {
+                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgValu, 80 / (2 * kS), 0);
+                __builtin_amdgcn_sched_group_barrier(kSgTrans, 32 / (2 * kS), 0);
+            }
+#pragma unroll
+            for (int x = 0; x < 4 * kB; ++x) {
+                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+            }
         }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s[b] = ahead[b];
     };
-    if (tiles.n > 0) issue(tiles[0], 0);
+    if (tiles.n > 0) {
+        issue_k(tiles[0], 0);
+        issue_v(tiles[0], 0);
+        if (tiles.n > 1) issue_k(tiles[1], 1);
+        wait_loads<0>();
+        barrier();
+        clear(s);
+#pragma unroll
+        for (int x = 0; x < kS; ++x) score(sK, x, s);
+    }
     while (i < tiles.n) {
         turn(std::integral_constant<int, 0>{});
         if (i >= tiles.n) break;
@@ -492,31 +535,33 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
     }
     int rb = top - skip, left = n;
     // One tile, in a buffer that is known when this is compiled, so that the addresses
-    // of all reads are a few registers and constants.
-    auto turn = [&](auto buffer) {
+    // of all reads are a few registers and constants.  With heads of 64 dP's products run
+    // between the exponentials, dV's between what makes dS of them; heads of 128 have no
+    // registers for dP that early.
+    constexpr bool EARLY = DT == 64;
+    auto work = [&](auto buffer, auto masked, int r0) {
         constexpr int B = decltype(buffer)::value;
-        wait_loads<0>();
-        barrier();
-        if (left > 1) issue(B ^ 1);
-        const int r0 = rb;
-        rb = rb > from * kQ ? rb - kQ : top;
-        if (r0 + kQ <= some_lo || r0 >= some_hi) return;
-        const bool all = r0 >= all_lo && r0 + kQ <= all_hi;
         const uint8_t *tq = sQ + B * kTile, *td = sD + B * kTile, *tv = sV + wave * (32 * DT * 2);
         const float* tr = sR + B * 64 + 4 * h;
+        const int lo = first - r0 - 4 * h, hi = last - r0 - 4 * h;
         f32x16 s, t;
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = t[e] = 0.0f;
 #pragma unroll
         for (int x = 0; x < kS; ++x) s = product32<T>(read_along<DT>(tq, 0, x, lane), k[x], s);
+        auto dp = [&]() {
+#pragma unroll
+            for (int x = 0; x < kS; ++x)
+                t = product32<T>(read_along<DT>(td, 0, x, lane), read_along<DT>(tv, 0, x, lane), t);
+        };
+        if (EARLY) dp();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const f32x4 ref = *(const f32x4*)(tr + 32 + 8 * e);
 #pragma unroll
             for (int y = 0; y < 4; ++y) s[4 * e + y] = exp2_fast(fmaf(s[4 * e + y], c, -ref[y]));
         }
-        const int lo = first - r0 - 4 * h, hi = last - r0 - 4 * h;
-        if (!all) {
+        if (masked) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = 8 * (e / 4) + e % 4;
@@ -531,16 +576,14 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
 #pragma unroll
             for (int y = 0; y < kB; ++y) dv[y] = product32<T>(read_across<DT>(td, 16 * x, y, lane), pt, dv[y]);
         }
-#pragma unroll
-        for (int x = 0; x < kS; ++x)
-            t = product32<T>(read_along<DT>(td, 0, x, lane), read_along<DT>(tv, 0, x, lane), t);
+        if (!EARLY) dp();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const f32x4 delta = *(const f32x4*)(tr + 8 * e);
 #pragma unroll
             for (int y = 0; y < 4; ++y) s[4 * e + y] *= t[4 * e + y] - delta[y];
         }
-        if (!all) {                                  // (0 times what is not finite)
+        if (masked) {                                // (0 times what is not finite)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = 8 * (e / 4) + e % 4;
@@ -555,6 +598,45 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
 #pragma unroll
             for (int y = 0; y < kB; ++y) dk[y] = product32<T>(read_across<DT>(tq, 16 * x, y, lane), ds, dk[y]);
         }
+        if (EARLY && !masked) {
+            __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+#pragma unroll
+            for (int x = 0; x < kS; ++x) {
+                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+#pragma unroll
+            for (int x = 0; x < kS; ++x) {
+                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgValu, 24 / kS, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgTrans, 16 / kS, 0);
+            }
+#pragma unroll
+            for (int x = 0; x < 2 * kB; ++x) {
+                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgValu, 40 / (2 * kB), 0);
+            }
+#pragma unroll
+            for (int x = 0; x < 2 * kB; ++x) {
+                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
+            }
+        }
+    };
+    auto turn = [&](auto buffer) {
+        wait_loads<0>();
+        barrier();
+        if (left > 1) issue(decltype(buffer)::value ^ 1);
+        const int r0 = rb;
+        rb = rb > from * kQ ? rb - kQ : top;
+        if (r0 + kQ <= some_lo || r0 >= some_hi) return;
+        const bool all = r0 >= all_lo && r0 + kQ <= all_hi;
+        if (!EARLY) work(buffer, !all, r0);
+        else if (all) work(buffer, std::false_type{}, r0);
+        else work(buffer, std::true_type{}, r0);
     };
     while (left > 0) {
         turn(std::integral_constant<int, 0>{});
