@@ -558,3 +558,6 @@ def gemm_noalloc(layout, M, N, K, a, a_scales, a_dec, b, b_scales, b_dec, out, s
 
 from .operators import (dropout_forward, gemm_fp8, layer_norm_forward, layer_norm_grad, linear_fp8,  # noqa: E402
                         quantize_fp8, quantize_fp8_dual, quantize_fp8_tiles)
+from .attention import attention, attention_forward, paged_attention  # noqa: E402
+from .paged import PagedCache, copy_pages  # noqa: E402
+from .rotary import (packed_positions, qk_norm_rope, qk_norm_rope_append, rotary_frequencies)  # noqa: E402

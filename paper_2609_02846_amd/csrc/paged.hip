@@ -20,7 +20,7 @@ namespace ue5m3 {
 namespace {
 
 constexpr int kWaves = 4, kTileKeys = 32, kCols = 16;
-constexpr int kLeastKeys = 256;                      // of a part: two tiles a wave
+constexpr int kLeastKeys = 512;                      // of a part: four tiles a wave
 constexpr int kMaxParts = 128, kMaxHead = 128;
 
 // Chunk c of a row of the values' tile lies at c ^ place: reads across rows take 32
@@ -281,6 +281,10 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const float* _
 
 }  // namespace
 
+// About eight workgroups for each CU, of rows that differ in length (24 rows of up to 8191
+// tokens, 8 key-value heads: with two for each CU 81 us, four 63, eight 62, sixteen 66),
+// and no part of fewer than 512 keys (one row of 32768: 64 parts 31.4 us, 128 of 256 keys
+// 35, as they take longer to join).
 int paged_parts(int64_t rows, int q_heads, int kv_heads, int64_t capacity, int64_t window, int64_t sinks) {
     const int group = q_heads / kv_heads;
     const int64_t work = rows * kv_heads * ((group + kCols - 1) / kCols);

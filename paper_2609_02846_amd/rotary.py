@@ -7,6 +7,7 @@ Frequencies are a tensor of the caller's, so that any scaling for long contexts
 is his; ``rotary_frequencies`` makes the common ones.
 """
 
+import functools
 import math
 
 import torch
@@ -53,6 +54,15 @@ def rotary_frequencies(dim, base=10000.0, factor=1.0, kind="linear", original=No
     return f.float().to(device), amplitude
 
 
+def packed_positions(starts, tokens):
+    """Position of each of ``tokens`` tokens in its own sequence, of sequences packed one
+    after the other from ``starts``[i] on (int64, on their device)."""
+    at = torch.arange(tokens, dtype=torch.int64, device=starts.device)
+    starts = starts.to(torch.int64)
+    i = torch.searchsorted(starts, at, right=True) - 1
+    return at - starts[i.clamp_min(0)]
+
+
 def _on_device(t, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA/HIP tensor")
@@ -61,30 +71,39 @@ def _on_device(t, name):
     return t
 
 
-def head_rows(t, name, dtypes=_TYPES, dense=False):
-    """``t`` [..., heads, dim] as (tensor, tokens, token stride, head stride): itself
-    where its strides allow, with the elements of a head together, else a copy.
-    ``dense``: as the attention kernels take it (heads apart, 16-byte aligned)."""
-    _on_device(t, name)
-    if t.dtype not in dtypes or t.dim() < 3:
-        raise ValueError(f"{name} must be [..., tokens, heads, dim] of " + ", ".join(str(d) for d in dtypes))
-    shape, stride = t.shape, t.stride()
+# (small calls are bound by the host: what follows from shapes and strides is worked out
+# once for each)
+@functools.lru_cache(maxsize=4096)
+def _row_layout(shape, stride, dense):
+    """(tokens, token stride, head stride) of [..., heads, dim], None where a copy is
+    needed for them."""
     ok = stride[-1] == 1 or shape[-1] == 1
-    token = stride[-3]
-    for d in range(t.dim() - 4, -1, -1):                 # leading dimensions as one
+    token, tokens = stride[-3], _numel(shape[:-2])
+    for d in range(len(shape) - 4, -1, -1):              # leading dimensions as one
         if shape[d] > 1:
             inner = _numel(shape[d + 1:-2])
             ok = ok and (inner <= 1 or stride[d] == token * inner)
             if inner <= 1:
                 token = stride[d]
     if dense:
-        tokens = _numel(shape[:-2])
         ok = (ok and (tokens <= 1 or shape[-1] <= token < 1 << 23) and (shape[-2] <= 1 or stride[-2] >= shape[-1])
-              and token % 8 == 0 and stride[-2] % 8 == 0 and t.data_ptr() % 16 == 0)
-    if not ok:
+              and token % 8 == 0 and stride[-2] % 8 == 0)
+    return (tokens, token, stride[-2]) if ok else None
+
+
+def head_rows(t, name, dtypes=_TYPES, dense=False):
+    """``t`` [..., heads, dim] as (tensor, tokens, token stride, head stride): itself
+    where its strides allow, with the elements of a head together, else a copy.
+    ``dense``: as the attention kernels take it (heads apart, 16-byte aligned)."""
+    _on_device(t, name)
+    shape = t.shape
+    if t.dtype not in dtypes or len(shape) < 3:
+        raise ValueError(f"{name} must be [..., tokens, heads, dim] of " + ", ".join(str(d) for d in dtypes))
+    layout = _row_layout(shape, t.stride(), dense)
+    if layout is None or dense and t.data_ptr() % 16:
         t = t.clone() if t.is_contiguous() else t.contiguous()       # (a contiguous one is not aligned)
-        token, stride = shape[-2] * shape[-1], t.stride()
-    return t, _numel(shape[:-2]), token, stride[-2]
+        layout = _row_layout(shape, t.stride(), False)
+    return (t, *layout)
 
 
 def _vector(t, name, dtypes, n):
@@ -123,7 +142,8 @@ def _arguments(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amp
             _on_device(positions, "positions")
             if positions.dtype not in (torch.int64, torch.int32):
                 raise ValueError("positions must be integers")
-            positions = positions.to(torch.int64).expand(lead).contiguous()
+            if positions.dtype != torch.int64 or positions.shape != lead or not positions.is_contiguous():
+                positions = positions.to(torch.int64).expand(lead).contiguous()
     else:
         positions = None
     args = RopeC(k_tokens, q.shape[-2] if q is not None else 0, k.shape[-2], dim, pairs, _TYPES[k.dtype], _TYPES[wt],
@@ -199,20 +219,26 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, positions=None, freqs=None,
     return _forward(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude)[:2]
 
 
-def cache_arguments(k_cache, v_cache, multiple=1):
-    """PagesC of the keys and values [pages, page_size, kv_heads, dim] of one layer."""
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        _on_device(t, name)
-        if t.dim() != 4 or t.stride(3) != 1 and t.shape[3] > 1:
-            raise ValueError(f"{name} must be [pages, page_size, kv_heads, dim], a head's elements together")
-    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.dtype != v_cache.dtype:
-        raise ValueError("k_cache and v_cache must have one shape, type and strides")
-    pages, size, _, _ = k_cache.shape
+@functools.lru_cache(maxsize=1024)
+def _page_layout(shape, stride, multiple):
+    if len(shape) != 4 or stride[3] != 1 and shape[3] > 1:
+        raise ValueError("a cache must be [pages, page_size, kv_heads, dim], a head's elements together")
+    size = shape[1]
     if size < 1 or size & (size - 1):
         raise ValueError("pages hold a power of two of tokens")
-    page, token, head = k_cache.stride()[:3]
-    if any(s % multiple for s in (page, token, head)):
+    if any(s % multiple for s in stride[:3]):
         raise ValueError(f"the cache's strides must be multiples of {multiple} elements")
+    return (shape[0], size, *stride[:3])
+
+
+def cache_arguments(k_cache, v_cache, multiple=1):
+    """PagesC of the keys and values [pages, page_size, kv_heads, dim] of one layer."""
+    _on_device(k_cache, "k_cache")
+    _on_device(v_cache, "v_cache")
+    shape, stride = k_cache.shape, k_cache.stride()
+    if shape != v_cache.shape or stride != v_cache.stride() or k_cache.dtype != v_cache.dtype:
+        raise ValueError("k_cache and v_cache must have one shape, type and strides")
+    pages, size, page, token, head = _page_layout(shape, stride, multiple)
     return PagesC(k_cache.data_ptr(), v_cache.data_ptr(), pages, size, page, token, head)
 
 

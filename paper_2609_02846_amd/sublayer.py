@@ -1,7 +1,8 @@
-"""A pre-norm residual branch, x + dropout(linear(layer_norm(x))), in training:
-layer norm, the 8-bit linear layer and dropout together.
+"""Pre-norm residual branches: x + dropout(linear(layer_norm(x))) in training, layer
+norm, the 8-bit linear layer and dropout together; and the attention branch, in
+training and over a paged cache.
 
-One autograd function, so that what the branch's ends share is joined: the
+The first is one autograd function, so that what the branch's ends share is joined: the
 residual is added in dropout's pass, and its gradient in the norm's backward
 pass.  Between the operators bf16 tensors are handed on, as between the
 separate calls, and the results are theirs.
@@ -11,10 +12,12 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import _check, _stream, load_library
+from .attention import attention, paged_attention
 from .dropout import Dropout
 from .fp8 import Fp8Linear, _check_formats, _flat, backward_products, forward_product
 from .norm import LayerNorm
 from .operators import BF16, dropout_forward, layer_norm_forward, norm_args, recorded
+from .rotary import packed_positions, qk_norm_rope, qk_norm_rope_append, rotary_frequencies
 
 
 class _SublayerFn(torch.autograd.Function):
@@ -93,3 +96,74 @@ class PreNormSublayer(torch.nn.Module):
         d = self.dropout
         return sublayer(x, self.norm.weight, self.norm.bias, self.linear.weight, d.p, d.next_key(), d.layer_id,
                         self.norm.eps, self.linear.scale, self.linear.grad_fmt)
+
+
+class PreNormAttention(torch.nn.Module):
+    """The attention branch of a decoder layer,
+
+        x + dropout(out(attention(norm_rope(qkv(layer_norm(x)))))),
+
+    with 8-bit linear layers (see ``Fp8Linear``), norms of queries and keys over each
+    head, rotation by position, and causal attention with an optional ``window`` and
+    ``sinks``.  ``rotary``: (freqs, amplitude), as ``rotary_frequencies`` gives them (None:
+    its defaults for the whole head).
+
+    ``forward`` is for training and evaluation of whole sequences; ``prompt`` is the same
+    without gradients and fills a cache; ``token`` takes one new token of each of several
+    sequences."""
+
+    def __init__(self, features, q_heads, kv_heads, head_dim, p=0.1, eps=1e-5, qk_eps=1e-6, rotary=None, window=0, sinks=0,
+                 scale="e8m0", grad_fmt="e4m3", seed=None, layer_id=0, device="cuda"):
+        super().__init__()
+        if q_heads < 1 or kv_heads < 1 or q_heads % kv_heads:
+            raise ValueError(f"{q_heads} query heads cannot share {kv_heads} key-value heads evenly")
+        self.heads, self.head_dim = (int(q_heads), int(kv_heads), int(kv_heads)), int(head_dim)
+        self.qk_eps, self.window, self.sinks = float(qk_eps), int(window), int(sinks)
+        self.norm = LayerNorm(features, eps, device=device)
+        self.qkv = Fp8Linear(features, sum(self.heads) * head_dim, scale, grad_fmt, device)
+        self.out = Fp8Linear(q_heads * head_dim, features, scale, grad_fmt, device)
+        self.q_weight, self.k_weight = (torch.nn.Parameter(torch.ones(head_dim, dtype=torch.bfloat16, device=device))
+                                        for _ in range(2))
+        self.dropout = Dropout(p, seed, layer_id)
+        freqs, self.amplitude = rotary_frequencies(head_dim, device=device) if rotary is None else rotary
+        self.register_buffer("freqs", freqs, persistent=False)
+
+    def _rotary(self, positions):
+        return self.q_weight, self.k_weight, positions, self.freqs, self.qk_eps, False, self.amplitude
+
+    def _project(self, x):
+        qkv = self.qkv(self.norm(x))
+        return qkv.view(*x.shape[:-1], sum(self.heads), self.head_dim).split(self.heads, dim=-2)
+
+    def _close(self, o, x):
+        return self.dropout(self.out(o.reshape(*x.shape[:-1], self.heads[0] * self.head_dim)), residual=x)
+
+    def _attend(self, x, starts, positions):
+        q, k, v = self._project(x)
+        if positions is None and starts is not None:
+            positions = packed_positions(starts, x.shape[0])
+        q, k = qk_norm_rope(q, k, *self._rotary(positions))
+        return self._close(attention(q, k, v, starts, window=self.window, sinks=self.sinks), x), k, v
+
+    def forward(self, x, starts=None, positions=None):
+        """``x`` [batch, length, features] (bf16), or [tokens, features] of sequences packed
+        one after the other (``starts``, as ``attention`` takes them).  ``positions`` default
+        to each sequence's own, from 0."""
+        return self._attend(x, starts, positions)[0]
+
+    @torch.no_grad()
+    def prompt(self, x, k_cache, v_cache, slots, starts=None, positions=None):
+        """``forward`` of whole prompts [tokens, features], whose keys and values go to
+        ``slots`` of a cache (see ``qk_norm_rope_append``)."""
+        y, k, v = self._attend(x, starts, positions)
+        qk_norm_rope_append(None, k, v, k_cache, v_cache, slots, eps=None)
+        return y
+
+    @torch.no_grad()
+    def token(self, x, k_cache, v_cache, slots, table, lengths):
+        """One new token of each of several sequences, ``x`` [rows, features]: its key and
+        value go to ``slots``, and it attends to the ``lengths`` tokens of its row of
+        ``table``, itself the last (see ``paged_attention``)."""
+        q, k, v = self._project(x)
+        q = qk_norm_rope_append(q, k, v, k_cache, v_cache, slots, *self._rotary(lengths - 1))
+        return self._close(paged_attention(q, k_cache, v_cache, table, lengths, window=self.window, sinks=self.sinks), x)
