@@ -92,6 +92,16 @@ __device__ __forceinline__ void load_operand(u32x4 (&f)[DT / 16], const void* ro
     }
 }
 
+// Whether the two numbers of a word are not finite: bits 15 and 31 of the result.
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    constexpr uint32_t kExponent = std::is_same_v<T, bf16> ? 0x7F807F80u : 0x7C007C00u;
+    return (w & kExponent) + (std::is_same_v<T, bf16> ? 0x00800080u : 0x04000400u);
+}
+
+// The n lowest bits.
+__device__ __forceinline__ uint64_t below(int n) { return n >= 64 ? ~(uint64_t)0 : n <= 0 ? 0 : ((uint64_t)1 << n) - 1; }
+
 // A transposed accumulator's column (a lane pair's row of the tensor) times f.
 template <typename T, int DT>
 __device__ __forceinline__ void store_column(T* row, const f32x16 (&o)[DT / 32], float f, int dim) {
@@ -126,6 +136,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
     constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
     __shared__ __attribute__((aligned(16))) uint8_t sK[2 * kTile];
     __shared__ __attribute__((aligned(16))) uint8_t sV[2 * kTile];
+    __shared__ uint32_t sSpoilt[2][2];               // keys of a tile whose values are not all finite
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
     const int head = head_of(blockIdx.x, a.q_heads, a.kv_heads), kv = head / (a.q_heads / a.kv_heads);
     const Span w = find_span<kRows, false, true>((int)(blockIdx.x / a.q_heads), a.sequences, a.q_starts, a.k_starts,
@@ -142,6 +153,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
     const Sight sees = sight(a, w.keys);
     const KeyTiles tiles(sees, r0 + off, min(r0 + kRows, w.rows) - 1 + off);
     const WaveSight mine(sees, r0 + wave * 32 + off, min(r0 + wave * 32 + 31, w.rows - 1) + off);
+    const WaveSight ours(sees, r0 + off, min(r0 + kRows, w.rows) - 1 + off);     // the whole workgroup's
     const int last = sees.last(row + off), before = sees.before(row + off);
 
     u32x4 q[kS];
@@ -180,11 +192,40 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
 #pragma unroll
             for (int e = 0; e < 16; ++e) to[b][e] = 0.0f;
     };
+    // Of a tile that some rows see in part: 0 times a value that is not finite would reach
+    // rows that do not see it.  In LDS zeros take the place of such values, each wave's of what
+    // it loaded, and the rows that see one become NaN as a whole.
+    auto clean = [&](uint8_t* tv, uint32_t* spoilt, int j0) {
+        constexpr int kN = kTile / 4096;
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+            u32x4* const p = (u32x4*)(tv + (wave * kN + n) * 1024 + lane * 16);
+            u32x4 f = *p;
+            uint32_t any = 0;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const uint32_t e = not_finite<T>(f[y]) >> 15 & 0x00010001u;
+                any |= e;
+                f[y] &= ~(e * 0xFFFFu);
+            }
+            if (any != 0) {
+                const int key = (wave * kN + n) * (1024 / (2 * DT)) + lane / (DT / 8);
+                atomicOr(&spoilt[key / 32], 1u << key % 32);
+                *p = f;
+            }
+        }
+        barrier();
+        const uint64_t keys = (uint64_t)spoilt[1] << 32 | spoilt[0];
+        if (keys != 0) {
+            const uint64_t seen = below(last - j0 + 1) & (~below(before - j0 + 1) | below(sees.sinks - j0));
+            if ((keys & seen) != 0) sum = __builtin_nanf("");
+        }
+    };
     // One tile: its scores are there, and the next one's are computed between its
     // exponentials.  The buffer is known when this is compiled, so that the addresses of
     // all reads are a few registers and constants.
     int i = 0;
-    auto turn = [&](auto buffer) {
+    auto turn = [&](auto buffer) __attribute__((always_inline)) {
         constexpr int B = decltype(buffer)::value;   // of this tile's values, and the tile's after the next keys
         wait_loads<0>();
         barrier();
@@ -193,6 +234,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
         if (i + 1 < tiles.n) issue_k(tiles[i + 1], B);
         if (i < tiles.n) issue_v(tiles[i], B ^ 1);
         const uint8_t *tk = sK + (B ^ 1) * kTile, *tv = sV + B * kTile;
+        if (threadIdx.x < 2) sSpoilt[B ^ 1][threadIdx.x] = 0;       // (of the last turn: all waves have read it)
+        if (!ours.all(j0)) clean(sV + B * kTile, sSpoilt[B], j0);
         f32x16 ahead[2];
         clear(ahead);
         if (mine.none(j0)) {
@@ -211,8 +254,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
 #pragma unroll
             for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
             top = fmaxf(top, other_half(top)) * c;
-            if (__ballot(top > m + kSlack) != 0) {
-                const float next = fmaxf(m, top), f = exp2_fast(m - next);
+            if (__ballot(top > m + kSlack) != 0) {   // (each row by itself: none depends on its neighbours)
+                const float next = top > m + kSlack ? top : m, f = exp2_fast(m - next);
                 const float scale = m == next ? 1.0f : f;
                 m = next;
                 sum *= scale;
@@ -257,6 +300,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
 #pragma unroll
         for (int b = 0; b < 2; ++b) s[b] = ahead[b];
     };
+    if (threadIdx.x < 4) sSpoilt[threadIdx.x / 2][threadIdx.x % 2] = 0;
     if (tiles.n > 0) {
         issue_k(tiles[0], 0);
         issue_v(tiles[0], 0);
@@ -287,11 +331,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
 }
 
 // dQ, and the rows' sums do . o, which both halves of the backward pass take.
-// As the forward kernel; P is exp(score - lse) and dS = P (dP - do . o) is rounded to
-// the inputs' type for its product.  dP and do . o often nearly cancel, so the rounding of
-// o would be the largest error of dS: the forward pass keeps what it left (with it dQ
-// and dK of 8192 tokens are 2.5e-3 from the exact ones in relative L2 norm, 1.7e-3 of
-// which their own rounding makes; without it 3.4e-3).
+// As the forward kernel; P is exp(score - lse) and dS = P (dP - do . o) goes to its
+// product as two numbers of the inputs' type, its rounding and the rounding of what that
+// left (one product more for each operand read: 8% of a training step).  dP and
+// do . o often nearly cancel, so the rounding of o would be the largest error of dS: the
+// forward pass keeps what it left, too.  In relative L2 norm dQ and dK of 8192 tokens are
+// 1.9e-3 and 2.4e-3 from the exact ones, 1.7e-3 of which their own rounding makes; with
+// dS in one number dQ is 2.6e-3 off, with o as it was rounded 3.4e-3.
 template <typename T, int DT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items) {
     constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
@@ -359,7 +405,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
     const float c = a.scale * kLog2e;
 
     int i = 0;
-    auto turn = [&](auto buffer) {
+    auto turn = [&](auto buffer) __attribute__((always_inline)) {
         constexpr int B = decltype(buffer)::value;
         wait_loads<0>();
         barrier();
@@ -387,11 +433,20 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
             }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                u32x4 ds;
+                u32x4 ds, rest;
 #pragma unroll
-                for (int y = 0; y < 4; ++y) ds[y] = pack2<T>(s[8 * x + 2 * y], s[8 * x + 2 * y + 1]);
+                for (int y = 0; y < 4; ++y) {
+                    const float u = s[8 * x + 2 * y], v = s[8 * x + 2 * y + 1];
+                    ds[y] = pack2<T>(u, v);
+                    const float2 r = unpack2<T>(ds[y]);
+                    rest[y] = pack2<T>(u - r.x, v - r.y);
+                }
 #pragma unroll
-                for (int y = 0; y < kB; ++y) dq[y] = product32<T>(read_across<DT>(tk, 32 * b + 16 * x, y, lane), ds, dq[y]);
+                for (int y = 0; y < kB; ++y) {
+                    const u32x4 f = read_across<DT>(tk, 32 * b + 16 * x, y, lane);
+                    dq[y] = product32<T>(f, ds, dq[y]);
+                    dq[y] = product32<T>(f, rest, dq[y]);
+                }
             }
         }
     };
@@ -539,7 +594,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
     // between the exponentials, dV's between what makes dS of them; heads of 128 have no
     // registers for dP that early.
     constexpr bool EARLY = DT == 64;
-    auto work = [&](auto buffer, auto masked, int r0) {
+    auto work = [&](auto buffer, auto masked, int r0) __attribute__((always_inline)) {
         constexpr int B = decltype(buffer)::value;
         const uint8_t *tq = sQ + B * kTile, *td = sD + B * kTile, *tv = sV + wave * (32 * DT * 2);
         const float* tr = sR + B * 64 + 4 * h;
@@ -626,7 +681,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
             }
         }
     };
-    auto turn = [&](auto buffer) {
+    auto turn = [&](auto buffer) __attribute__((always_inline)) {
         wait_loads<0>();
         barrier();
         if (left > 1) issue(decltype(buffer)::value ^ 1);

@@ -139,6 +139,27 @@ def test_tokens_of_no_sequence():
     assert torch.equal(one, attention(q.detach(), k.detach(), v.detach()))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D", [64, 128, 40])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_what_is_not_seen_does_not_matter(bad, D, dtype):
+    """Keys and values that are not finite change the rows that see them only."""
+    L, H = 200, 2
+    q, k, v = (rand(i, L, n, D, dtype=dtype) for i, n in ((0, H), (1, 1), (2, 1)))
+    for window, sinks, at in ((0, 0, [70]), (0, 0, [199]), (0, 0, [64, 130]), (50, 0, [0, 60]), (20, 70, [10, 66, 150]), (30, 3, [2, 5])):
+        want = attention(q, k, v, window=window, sinks=sinks)
+        sees = model.visible(L, L, True, window, sinks)[:, at].any(1)
+        for where in ("k", "v", "kv"):
+            k2, v2 = k.clone(), v.clone()
+            for t, n in ((k2, "k"), (v2, "v")):
+                if n in where:
+                    t[at, 0, D // 2] = bad
+            o = attention(q, k2, v2, window=window, sinks=sinks)
+            assert torch.equal(o[~sees], want[~sees]), (window, sinks, at, where)
+            if where == "v":
+                assert not torch.isfinite(o[sees]).all(-1).any(), (window, sinks, at)
+
+
 def test_differences():
     """The gradient along a direction against a difference of the 64-bit model, whose
     own gradient the kernel is held to above: the model's formula itself."""
