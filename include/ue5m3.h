@@ -736,7 +736,8 @@ ue5m3_status_t ue5m3_copy_pages(void* base, int64_t planes, int64_t plane, int64
  * all of it NaN.  lse [q_heads][q_tokens] (nullable) receives log(sum
  * of exp(s_j)), -inf for a query that sees nothing; o_rest (nullable, as o) what the
  * rounding left, rounded to `type` itself: the gradients need more of o than it holds.
- * Tokens of no sequence get zeros (lse -inf).  q, k and v have strides, o is dense
+ * Tokens of no sequence get zeros (lse -inf).  `scratch` has ue5m3_attention_scratch(args)
+ * bytes (null where that is 0).  q, k and v have strides, o is dense
  * [q_tokens][q_heads][dim].
  *
  * q, k, v, o and o_rest are 16-byte aligned, strides are multiples of 8 elements, dim is a
@@ -760,7 +761,8 @@ typedef struct {
     float* lse;
 } ue5m3_attention_t;
 
-ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, hipStream_t stream);
+int64_t ue5m3_attention_scratch(const ue5m3_attention_t* args);
+ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, void* scratch, hipStream_t stream);
 
 /*
  * Its gradients for the output gradient d_o (dense): with P = exp(s - lse) and

@@ -40,7 +40,7 @@ EXPORTED_SYMBOLS = (
     "ue5m3_layer_norm", "ue5m3_layer_norm_grad", "ue5m3_dropout",
     "ue5m3_quantize_fp8", "ue5m3_quantize_fp8_tiles", "ue5m3_gemm_fp8", "ue5m3_linear_fp8",
     "ue5m3_qk_norm_rope", "ue5m3_qk_norm_rope_grad", "ue5m3_qk_norm_rope_grad_scratch", "ue5m3_qk_norm_rope_append",
-    "ue5m3_copy_pages", "ue5m3_attention", "ue5m3_attention_grad", "ue5m3_attention_grad_scratch", "ue5m3_paged_attention",
+    "ue5m3_copy_pages", "ue5m3_attention", "ue5m3_attention_scratch", "ue5m3_attention_grad", "ue5m3_attention_grad_scratch", "ue5m3_paged_attention",
     "ue5m3_paged_attention_scratch",
 )
 
@@ -198,7 +198,9 @@ def load_library(path=LIB_PATH):
     lib.ue5m3_qk_norm_rope_append.restype = i32
     lib.ue5m3_copy_pages.argtypes = [vp, i64, i64, i64, i64, ptr(i32), ptr(i32), i64, vp]
     lib.ue5m3_copy_pages.restype = i32
-    lib.ue5m3_attention.argtypes = [ptr(AttentionC), vp]
+    lib.ue5m3_attention_scratch.argtypes = [ptr(AttentionC)]
+    lib.ue5m3_attention_scratch.restype = i64
+    lib.ue5m3_attention.argtypes = [ptr(AttentionC), vp, vp]
     lib.ue5m3_attention.restype = i32
     lib.ue5m3_attention_grad_scratch.argtypes = [ptr(AttentionC)]
     lib.ue5m3_attention_grad_scratch.restype = i64

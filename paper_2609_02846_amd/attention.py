@@ -77,7 +77,10 @@ def attention_forward(q, k, v, q_starts=None, k_starts=None, scale=None, causal=
     if _rest:
         rest = torch.empty_like(o)
         args.o_rest = rest.data_ptr()
-    _check(load_library().ue5m3_attention(args, _stream()), "ue5m3_attention")
+    lib = load_library()
+    n = lib.ue5m3_attention_scratch(args)
+    scratch = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    _check(lib.ue5m3_attention(args, _ptr(scratch), _stream()), "ue5m3_attention")
     return (o, sums, rest) if _rest else (o, sums) if lse else o
 
 

@@ -85,7 +85,7 @@ ue5m3_status_t attention_args(const ue5m3_attention_t* a) {
         (int64_t)a->q_heads * a->dim >= kMaxStride)
         return UE5M3_ESHAPE;
     const bool ragged = a->q_starts != nullptr;
-    if (ue5m3::attention_items(a->q_tokens, a->sequences, ragged) > kMaxGrid / a->q_heads ||
+    if (ue5m3::attention_items(a->q_tokens, a->sequences, ragged) > kMaxGrid / 8 / a->q_heads ||
         ue5m3::attention_items(a->k_tokens, a->sequences, ragged) > kMaxGrid / 8 / a->kv_heads ||
         (a->q_tokens / 64 + 2) * (a->q_heads / a->kv_heads) > 0x7FFFFFFF)
         return UE5M3_ESHAPE;
@@ -96,6 +96,13 @@ ue5m3_status_t attention_args(const ue5m3_attention_t* a) {
         (a->q_token | a->q_head | a->k_token | a->k_head | a->v_token | a->v_head) % 8 != 0)
         return UE5M3_EALIGN;
     return UE5M3_OK;
+}
+
+// Whether the sizes that scratch memory goes by are such.
+bool sizes_ok(const ue5m3_attention_t* a) {
+    return a != nullptr && a->q_tokens >= 0 && a->q_tokens <= kMaxTokens && a->k_tokens >= 0 && a->k_tokens <= kMaxTokens &&
+           a->sequences >= 1 && a->q_heads >= 1 && a->q_heads <= kMaxHeads && a->kv_heads >= 1 && a->kv_heads <= a->q_heads &&
+           a->dim >= 1 && a->dim <= 128 && a->window >= 0 && a->sinks >= 0;
 }
 
 }  // namespace
@@ -177,17 +184,20 @@ ue5m3_status_t ue5m3_copy_pages(void* base, int64_t planes, int64_t plane, int64
     return status(ue5m3::launch_copy_pages(base, planes, plane, page, src, dst, n, stream));
 }
 
-ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, hipStream_t stream) {
+ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, void* scratch, hipStream_t stream) {
     const ue5m3_status_t st = attention_args(args);
     if (st != UE5M3_OK || args->q_tokens == 0) return st;
-    return status(ue5m3::launch_attention(*args, stream));
+    if (ue5m3::attention_scratch(*args) > 0 && scratch == nullptr) return UE5M3_EINVAL;
+    if (!aligned(scratch, 16)) return UE5M3_EALIGN;
+    return status(ue5m3::launch_attention(*args, (float*)scratch, stream));
+}
+
+int64_t ue5m3_attention_scratch(const ue5m3_attention_t* args) {
+    return sizes_ok(args) ? ue5m3::attention_scratch(*args) : 0;
 }
 
 int64_t ue5m3_attention_grad_scratch(const ue5m3_attention_t* args) {
-    return args == nullptr || args->q_tokens < 0 || args->k_tokens < 0 || args->q_tokens > kMaxTokens ||
-                   args->k_tokens > kMaxTokens || args->sequences < 1 || args->q_heads < 1 || args->kv_heads < 1 ||
-                   args->q_heads > kMaxHeads || args->kv_heads > kMaxHeads || args->dim < 1 || args->dim > 128
-               ? 0 : ue5m3::attention_grad_scratch(*args);
+    return sizes_ok(args) ? ue5m3::attention_grad_scratch(*args) : 0;
 }
 
 ue5m3_status_t ue5m3_attention_grad(const ue5m3_attention_t* args, const ue5m3_attention_grad_t* grad,

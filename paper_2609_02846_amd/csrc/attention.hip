@@ -117,41 +117,53 @@ __device__ __forceinline__ void store_column(T* row, const f32x16 (&o)[DT / 32],
 }
 
 // Rows of no sequence: zeros in this head's share of an output (each workgroup past
-// the tiles takes every `extras`-th row), and -inf for `lse`.
-template <typename T>
+// the tiles takes every `extras`-th row), and -inf for `lse`, or that and a sum of 0.
+__device__ __forceinline__ void empty_row(float& lse) { lse = -__builtin_inff(); }
+__device__ __forceinline__ void empty_row(float2& ml) { ml = make_float2(-__builtin_inff(), 0.0f); }
+template <typename T, typename L>
 __device__ __forceinline__ void clear_outside(T* out, int64_t token, const int32_t* starts, int64_t n, int64_t tokens,
-                                              int dim, int extra, int extras, float* lse) {
+                                              int dim, int extra, int extras, L* lse) {
     if (starts == nullptr) return;
     const int64_t before = min(max((int64_t)starts[0], (int64_t)0), tokens);
     const int64_t after = min(max((int64_t)starts[n], before), tokens);
     for (int64_t i = extra; i < before + tokens - after; i += extras) {
         const int64_t t = i < before ? i : after + i - before;
-        for (int d = threadIdx.x; d < dim; d += kAttnThreads) out[t * token + d] = (T)0.0f;
-        if (lse != nullptr && threadIdx.x == 0) lse[t] = -__builtin_inff();
+        if constexpr (!std::is_same_v<T, float2>)
+            for (int d = threadIdx.x; d < dim; d += kAttnThreads) out[t * token + d] = (T)0.0f;
+        if (lse != nullptr && threadIdx.x == 0) empty_row(lse[t]);
     }
 }
 
+// Of the forward call's scratch memory: the parts' outputs [parts][tokens][heads][dim],
+// then their rows' references and sums [parts][heads][tokens][2].
+__host__ __device__ inline int64_t o_floats(const ue5m3_attention_t& a) { return a.q_tokens * a.q_heads * a.dim; }
+
 template <typename T, int DT>
-__global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attention_t a, int items) {
+__global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attention_t a, int items, int parts, float* scratch) {
     constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
     __shared__ __attribute__((aligned(16))) uint8_t sK[2 * kTile];
     __shared__ __attribute__((aligned(16))) uint8_t sV[2 * kTile];
     __shared__ uint32_t sSpoilt[2][2];               // keys of a tile whose values are not all finite
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
     const int head = head_of(blockIdx.x, a.q_heads, a.kv_heads), kv = head / (a.q_heads / a.kv_heads);
-    const Span w = find_span<kRows, false, true>((int)(blockIdx.x / a.q_heads), a.sequences, a.q_starts, a.k_starts,
-                                                 a.q_tokens, a.k_tokens);
+    const int part = blockIdx.x / a.q_heads % parts, item = blockIdx.x / (a.q_heads * parts);
+    const Span w = find_span<kRows, false, true>(item, a.sequences, a.q_starts, a.k_starts, a.q_tokens, a.k_tokens);
+    // this head's part, and its rows' references and sums
+    float* const part_o = scratch + (int64_t)part * o_floats(a) + (int64_t)head * a.dim;
+    float2* const part_ml = (float2*)(scratch + parts * o_floats(a)) + ((int64_t)part * a.q_heads + head) * a.q_tokens;
     T* const o_head = (T*)a.o + (int64_t)head * a.dim;
     const int64_t o_token = (int64_t)a.q_heads * a.dim;
     float* const lse_head = a.lse != nullptr ? a.lse + head * a.q_tokens : nullptr;
     if (w.tile < 0) {
-        const int extras = items - ((int)(blockIdx.x / a.q_heads) - w.extra);
-        clear_outside(o_head, o_token, a.q_starts, a.sequences, a.q_tokens, a.dim, w.extra, extras, lse_head);
+        const int extras = items - (item - w.extra);
+        if (parts > 1) clear_outside((float2*)nullptr, 0, a.q_starts, a.sequences, a.q_tokens, 0, w.extra, extras, part_ml);
+        else clear_outside(o_head, o_token, a.q_starts, a.sequences, a.q_tokens, a.dim, w.extra, extras, lse_head);
         return;
     }
     const int off = w.keys - w.rows, r0 = w.tile * kRows, row = r0 + wave * 32 + (lane & 31);
     const Sight sees = sight(a, w.keys);
     const KeyTiles tiles(sees, r0 + off, min(r0 + kRows, w.rows) - 1 + off);
+    const int i0 = (int)((int64_t)tiles.n * part / parts), i1 = (int)((int64_t)tiles.n * (part + 1) / parts);
     const WaveSight mine(sees, r0 + wave * 32 + off, min(r0 + wave * 32 + 31, w.rows - 1) + off);
     const WaveSight ours(sees, r0 + off, min(r0 + kRows, w.rows) - 1 + off);     // the whole workgroup's
     const int last = sees.last(row + off), before = sees.before(row + off);
@@ -224,15 +236,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
     // One tile: its scores are there, and the next one's are computed between its
     // exponentials.  The buffer is known when this is compiled, so that the addresses of
     // all reads are a few registers and constants.
-    int i = 0;
+    int i = i0;
     auto turn = [&](auto buffer) __attribute__((always_inline)) {
         constexpr int B = decltype(buffer)::value;   // of this tile's values, and the tile's after the next keys
         wait_loads<0>();
         barrier();
         const int j0 = tiles[i] * kKeys;
         ++i;
-        if (i + 1 < tiles.n) issue_k(tiles[i + 1], B);
-        if (i < tiles.n) issue_v(tiles[i], B ^ 1);
+        if (i + 1 < i1) issue_k(tiles[i + 1], B);
+        if (i < i1) issue_v(tiles[i], B ^ 1);
         const uint8_t *tk = sK + (B ^ 1) * kTile, *tv = sV + B * kTile;
         if (threadIdx.x < 2) sSpoilt[B ^ 1][threadIdx.x] = 0;       // (of the last turn: all waves have read it)
         if (!ours.all(j0)) clean(sV + B * kTile, sSpoilt[B], j0);
@@ -301,23 +313,35 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
         for (int b = 0; b < 2; ++b) s[b] = ahead[b];
     };
     if (threadIdx.x < 4) sSpoilt[threadIdx.x / 2][threadIdx.x % 2] = 0;
-    if (tiles.n > 0) {
-        issue_k(tiles[0], 0);
-        issue_v(tiles[0], 0);
-        if (tiles.n > 1) issue_k(tiles[1], 1);
+    if (i0 < i1) {
+        issue_k(tiles[i0], 0);
+        issue_v(tiles[i0], 0);
+        if (i0 + 1 < i1) issue_k(tiles[i0 + 1], 1);
         wait_loads<0>();
         barrier();
         clear(s);
 #pragma unroll
         for (int x = 0; x < kS; ++x) score(sK, x, s);
     }
-    while (i < tiles.n) {
+    while (i < i1) {
         turn(std::integral_constant<int, 0>{});
-        if (i >= tiles.n) break;
+        if (i >= i1) break;
         turn(std::integral_constant<int, 1>{});
     }
     sum += other_half(sum);
     if (row >= w.rows) return;
+    if (parts > 1) {
+#pragma unroll
+        for (int b = 0; b < kB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int x = 32 * b + 8 * e + 4 * h;
+                if (x < a.dim)
+                    *(f32x4*)(part_o + (w.q0 + row) * o_token + x) = f32x4{o[b][4 * e], o[b][4 * e + 1], o[b][4 * e + 2], o[b][4 * e + 3]};
+            }
+        if (h == 0) part_ml[w.q0 + row] = make_float2(m, sum);
+        return;
+    }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     store_column<T, DT>(o_head + (w.q0 + row) * o_token, o, inv, a.dim);
     if (a.o_rest != nullptr) {
@@ -328,6 +352,40 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
         store_column<T, DT>((T*)a.o_rest + (w.q0 + row) * o_token + (int64_t)head * a.dim, o, 1.0f, a.dim);
     }
     if (lse_head != nullptr && h == 0) lse_head[w.q0 + row] = sum == 0.0f ? -__builtin_inff() : m * kLn2 + logf(sum);
+}
+
+// Outputs from the parts of the keys, in their order; a thread four elements.
+template <typename T>
+__global__ __launch_bounds__(kAttnThreads) void attention_join_kernel(ue5m3_attention_t a, int parts, const float* __restrict__ scratch) {
+    const int64_t n = o_floats(a), i = ((int64_t)blockIdx.x * kAttnThreads + threadIdx.x) * 4;
+    if (i >= n) return;
+    const int64_t row = i / a.dim, token = row / a.q_heads;
+    const int d = (int)(i - row * a.dim), head = (int)(row - token * a.q_heads);
+    const int64_t step = (int64_t)a.q_heads * a.q_tokens;
+    const float2* ml = (const float2*)(scratch + parts * n) + head * a.q_tokens + token;
+    float m = -__builtin_inff(), l = 0.0f;
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, ml[p * step].x);
+    const float ref = m == -__builtin_inff() ? 0.0f : m;
+    f32x4 v = {0, 0, 0, 0};
+    for (int p = 0; p < parts; ++p) {
+        const float2 x = ml[p * step];
+        const float f = exp2_fast(x.x - ref);
+        l += x.y * f;
+        v += *(const f32x4*)(scratch + p * n + i) * f;
+    }
+    const float inv = 1.0f / l;
+    u32x2 w, rest;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) v[y] = l == 0.0f ? 0.0f : v[y] * inv;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        w[y] = pack2<T>(v[2 * y], v[2 * y + 1]);
+        const float2 r = unpack2<T>(w[y]);
+        rest[y] = pack2<T>(v[2 * y] - r.x, v[2 * y + 1] - r.y);
+    }
+    __builtin_memcpy((T*)a.o + i, &w, 8);
+    if (a.o_rest != nullptr) __builtin_memcpy((T*)a.o_rest + i, &rest, 8);
+    if (a.lse != nullptr && d == 0) a.lse[head * a.q_tokens + token] = l == 0.0f ? -__builtin_inff() : m * kLn2 + logf(l);
 }
 
 // dQ, and the rows' sums do . o, which both halves of the backward pass take.
@@ -351,7 +409,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
         const int extras = items - ((int)(blockIdx.x / a.q_heads) - w.extra);
         if (g.dq != nullptr)
             clear_outside((T*)g.dq + head * g.dq_head, g.dq_token, a.q_starts, a.sequences, a.q_tokens, a.dim, w.extra,
-                          extras, nullptr);
+                          extras, (float*)nullptr);
         return;
     }
     const int off = w.keys - w.rows, r0 = w.tile * kRows, row = r0 + wave * 32 + (lane & 31);
@@ -496,11 +554,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
     if (w.tile < 0) {
         const int extras = items - (item - w.extra);
         if (parts > 1) {
-            clear_outside(part_dk, token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
-            clear_outside(part_dv, token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+            clear_outside(part_dk, token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, (float*)nullptr);
+            clear_outside(part_dv, token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, (float*)nullptr);
         } else {
-            clear_outside(dk_head, g.dk_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
-            clear_outside(dv_head, g.dv_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, nullptr);
+            clear_outside(dk_head, g.dk_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, (float*)nullptr);
+            clear_outside(dv_head, g.dv_token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, (float*)nullptr);
         }
         return;
     }
@@ -752,12 +810,34 @@ int64_t attention_items(int64_t tokens, int64_t sequences, bool ragged) {
     return ragged ? tokens / kRows + sequences + 1 : sequences * ((tokens / sequences + kRows - 1) / kRows);
 }
 
-hipError_t launch_attention(const ue5m3_attention_t& a, hipStream_t s) {
+// Parts that the keys of a query tile are cut into: two workgroups for each CU where there
+// are fewer tiles than that, and 8 tiles of keys for each by the sequences' mean length
+// (777 queries over 5001 keys, 32 heads: one part @Q1@ us, two @Q2@ with their joining).
+int attention_parts(const ue5m3_attention_t& a) {
+    if (a.q_tokens == 0 || a.k_tokens == 0) return 1;
+    const int64_t work = std::max<int64_t>((a.q_tokens + kRows - 1) / kRows, a.sequences) * a.q_heads;
+    int64_t keys = a.k_tokens / a.sequences;
+    if (a.causal && a.window != 0) keys = std::min(keys, std::min(a.window, keys) + std::min(a.sinks, keys) + kRows);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({8, 2 * kCus / work, keys / (8 * kKeys)}));
+}
+
+int64_t attention_scratch(const ue5m3_attention_t& a) {
+    const int parts = attention_parts(a);
+    return parts > 1 ? parts * (o_floats(a) + 2 * a.q_heads * a.q_tokens) * 4 : 0;
+}
+
+hipError_t launch_attention(const ue5m3_attention_t& a, float* scratch, hipStream_t s) {
     const int64_t items = attention_items(a.q_tokens, a.sequences, a.q_starts != nullptr);
+    const int parts = attention_parts(a);
     return with_head((DType)a.type, a.dim, [&](auto* t, auto d) {
         using T = std::remove_pointer_t<decltype(t)>;
-        hipLaunchKernelGGL((attention_kernel<T, decltype(d)::value>), dim3((unsigned)(items * a.q_heads)), dim3(kAttnThreads),
-                           0, s, a, (int)items);
+        hipLaunchKernelGGL((attention_kernel<T, decltype(d)::value>), dim3((unsigned)(items * parts * a.q_heads)),
+                           dim3(kAttnThreads), 0, s, a, (int)items, parts, scratch);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || parts == 1) return e;
+        const int64_t threads = (o_floats(a) + 3) / 4;
+        hipLaunchKernelGGL((attention_join_kernel<T>), dim3((unsigned)((threads + kAttnThreads - 1) / kAttnThreads)),
+                           dim3(kAttnThreads), 0, s, a, parts, scratch);
         return hipGetLastError();
     });
 }

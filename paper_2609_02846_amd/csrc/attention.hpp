@@ -34,7 +34,8 @@ hipError_t launch_copy_pages(void* base, int64_t planes, int64_t plane, int64_t 
 
 // Workgroups' tiles of all sequences, at most.
 int64_t attention_items(int64_t tokens, int64_t sequences, bool ragged);
-hipError_t launch_attention(const ue5m3_attention_t& a, hipStream_t s);
+int64_t attention_scratch(const ue5m3_attention_t& a);               // bytes
+hipError_t launch_attention(const ue5m3_attention_t& a, float* scratch, hipStream_t s);
 int64_t attention_grad_scratch(const ue5m3_attention_t& a);          // bytes
 hipError_t launch_attention_grad(const ue5m3_attention_t& a, const ue5m3_attention_grad_t& g, hipStream_t s);
 

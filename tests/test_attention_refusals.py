@@ -129,10 +129,20 @@ BAD_ATTENTION = BAD_HEADS + [
 
 
 def test_attention(lib):
-    assert lib.ue5m3_attention(attention_args(), None) == OK and lib.ue5m3_attention(None, None) == EINVAL
-    assert lib.ue5m3_attention(attention_args(q_starts=None, k_starts=None, sequences=3), None) == OK
+    assert lib.ue5m3_attention(attention_args(), None, None) == OK and lib.ue5m3_attention(None, None, None) == EINVAL
+    assert lib.ue5m3_attention(attention_args(q_starts=None, k_starts=None, sequences=3), None, None) == OK
     for kw, want in BAD_ATTENTION:
-        assert lib.ue5m3_attention(attention_args(**kw), None) == want, kw
+        assert lib.ue5m3_attention(attention_args(**kw), None, None) == want, kw
+
+
+def test_attention_scratch(lib):
+    few = dict(q_tokens=100, k_tokens=5000)
+    n = lib.ue5m3_attention_scratch
+    assert n(attention_args(**few)) > 0 and n(attention_args(q_tokens=100, k_tokens=100)) == 0 and n(None) == 0
+    assert n(attention_args(q_tokens=-1, k_tokens=5000)) == 0 and n(attention_args(window=-1, **few)) == 0
+    assert lib.ue5m3_attention(attention_args(**few), None, None) == EINVAL
+    assert lib.ue5m3_attention(attention_args(**few), HALF, None) == EALIGN
+    assert lib.ue5m3_attention_grad_scratch(attention_args(**few)) >= 2 * 4 * 100 * 4
 
 
 def test_attention_grad(lib):

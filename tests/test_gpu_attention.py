@@ -190,6 +190,22 @@ def test_same_bits_and_some_gradients():
         assert torch.equal(g, runs[0][1 + i])
 
 
+@pytest.mark.parametrize("mask", [{}, dict(causal=False), dict(window=900, sinks=70), dict(window=3000, sinks=0)])
+def test_keys_in_parts(mask):
+    """Few queries over many keys: their parts joined, with rows of no sequence and rows
+    whose parts see nothing."""
+    check([100], [3000], 2, 1, 128, torch.bfloat16, True, **mask)
+    check([1], [2049], 4, 2, 64, torch.float16, False, **mask)
+    check([130, 0, 3], [2600, 700, 1700], 2, 2, 64, torch.bfloat16, True, **mask)
+    check([200], [1100], 1, 1, 80, torch.bfloat16, True, **mask)
+    q, k, v = rand(1, 50, 2, 64), rand(2, 4000, 1, 64), rand(3, 4000, 1, 64)
+    s, t = torch.tensor([3, 40], dtype=torch.int32).cuda(), torch.tensor([0, 4000], dtype=torch.int32).cuda()
+    o, lse = attention_forward(q, k, v, s, t, lse=True, **mask)
+    assert not o[:3].any() and not o[40:].any() and (lse[:, 40:] == -float("inf")).all()
+    whole = model.Sequence(q[3:40], k, v, 64 ** -0.5, **mask)
+    model.within(o[3:40], whole.o.transpose(0, 1), whole.o_bound().transpose(0, 1), "inner")
+
+
 def test_empty():
     q, k = rand(0, 0, 2, 64).requires_grad_(), rand(1, 5, 2, 64).requires_grad_()
     o = attention(q, k, k.detach().requires_grad_(), starts([0]), starts([5]))
