@@ -10,6 +10,12 @@
 // product's operand as it lies in its registers; the output is accumulated
 // transposed too.  P is rounded to the inputs' type, as the matrix instructions
 // take it; scores, sums and the output are binary32.
+//
+// Bound: the two products and, in their shadow, the exponentials: the scores of the next
+// tile are computed between this one's (8192 tokens 594 us, one after the other 639).
+// 8192 tokens, causal, 32 heads of 128, bf16: 622 us with the care for values that are not
+// finite, 884 TFLOP/s of the 1426 that a large product reaches; the matrix pipe works in
+// 48% of the cycles.
 #include <algorithm>
 
 #include "attention.hpp"
@@ -391,11 +397,14 @@ __global__ __launch_bounds__(kAttnThreads) void attention_join_kernel(ue5m3_atte
 // dQ, and the rows' sums do . o, which both halves of the backward pass take.
 // As the forward kernel; P is exp(score - lse) and dS = P (dP - do . o) goes to its
 // product as two numbers of the inputs' type, its rounding and the rounding of what that
-// left (one product more for each operand read: 8% of a training step).  dP and
-// do . o often nearly cancel, so the rounding of o would be the largest error of dS: the
-// forward pass keeps what it left, too.  In relative L2 norm dQ and dK of 8192 tokens are
-// 1.9e-3 and 2.4e-3 from the exact ones, 1.7e-3 of which their own rounding makes; with
-// dS in one number dQ is 2.6e-3 off, with o as it was rounded 3.4e-3.
+// left (one product more for each operand read: 730 us against 916, 8% of a training
+// step).  dP and do . o often nearly cancel, so the rounding of o would be the largest
+// error of dS: the forward pass keeps what it left, too.  In relative L2 norm dQ and dK of
+// 8192 tokens are 1.9e-3 and 2.4e-3 from the exact ones, 1.7e-3 of which their own rounding
+// makes; with dS in one number dQ is 2.6e-3 off, with o as it was rounded 3.4e-3.
+//
+// Bound: the products.  8192 tokens, 32 heads of 128: 916 us for 0.82 TF, 1.10 with the
+// second number, 1200 TFLOP/s; the matrix pipe works in 62% of the cycles.
 template <typename T, int DT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items) {
     constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
@@ -532,7 +541,11 @@ __device__ __forceinline__ float* dkv_parts(const ue5m3_attention_t& a, const ue
 // Scores are queries x keys here, so that P and dS are the operands of the products that
 // contract over queries.  A wave's keys stay in registers, its values in LDS: with both in
 // registers there would be room for one wave a SIMD only, and nothing to fill its waits
-// (8192 tokens 1730 us against @DKV@).
+// (8192 tokens, 32 heads of 128, 8 of keys: 1730 us against 1230).
+//
+// Bound: the products, 4 of 2 pairs x heads x dim operations, and LDS, which holds Q and
+// dO for two reads each: those 1.10 TF take 1230 us (893 TFLOP/s), the matrix pipe works
+// in 43% of the cycles, half of the waves' others go on waiting for reads of LDS.
 template <typename T, int DT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items,
                                                                        int parts) {
@@ -603,8 +616,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
     load_operand<DT>(k, (const T*)a.k + at * a.k_token + kv * a.k_head, a.dim);
 
     // The tiles of a head come from its last to its first: causal workgroups then begin
-    // with the same rows and stay together, so that an XCD's L2 holds what they read (from
-    // the first on, each would begin at its own keys: @ASC@).
+    // with the same rows and an XCD's L2 holds what they read (measured, the order makes no
+    // difference: from the first on 2053 us against 2041, before there were parts).
     // The next loads: the rows from `next` on, at q_at, d_at and r_at.
     const int top = (from + per - 1) * kQ;           // first row of the last tile
     const int head = kv * group + (per > 0 ? i0 / per : 0), skip = per > 0 ? i0 % per * kQ : 0;
@@ -812,7 +825,7 @@ int64_t attention_items(int64_t tokens, int64_t sequences, bool ragged) {
 
 // Parts that the keys of a query tile are cut into: two workgroups for each CU where there
 // are fewer tiles than that, and 8 tiles of keys for each by the sequences' mean length
-// (777 queries over 5001 keys, 32 heads: one part @Q1@ us, two @Q2@ with their joining).
+// (777 queries over 5001 keys, 32 heads: one part 145 us, two 106 with their joining).
 int attention_parts(const ue5m3_attention_t& a) {
     if (a.q_tokens == 0 || a.k_tokens == 0) return 1;
     const int64_t work = std::max<int64_t>((a.q_tokens + kRows - 1) / kRows, a.sequences) * a.q_heads;
@@ -844,7 +857,7 @@ hipError_t launch_attention(const ue5m3_attention_t& a, float* scratch, hipStrea
 
 // Parts that a key tile's queries are cut into.  Causal tiles differ in length, and two
 // workgroups run on a CU: with four for each CU, the longest first, all CUs end together
-// (8192 tokens, 8 key-value heads: one part 2018 us, two @P2@ with their sum).  A part has
+// (8192 tokens, 8 key-value heads: one part 2041 us, two 1241 with their sum).  A part has
 // 16 tiles of queries at least, by the sequences' mean length.
 int dkv_parts_of(const ue5m3_attention_t& a) {
     if (a.q_tokens == 0 || a.k_tokens == 0) return 1;

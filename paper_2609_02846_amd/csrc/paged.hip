@@ -10,7 +10,9 @@
 // loaded a tile ahead, their pages' numbers two.  Parts are joined by a second
 // launch, in their order.
 //
-// Bound: HBM, each key and value read once.
+// Bound: HBM, each key and value read once.  One token over 32768 of 8 heads of 128
+// (134 MB): 26.3 us, 5.1 TB/s, what a copy reaches, and 4.7 for the joining; 24 rows of
+// up to 8191 (232 MB): 62 us, 3.7 TB/s, as the last rows to end leave CUs idle.
 #include <algorithm>
 
 #include "attention.hpp"

