@@ -87,7 +87,7 @@ ue5m3_status_t attention_args(const ue5m3_attention_t* a) {
     const bool ragged = a->q_starts != nullptr;
     if (ue5m3::attention_items(a->q_tokens, a->sequences, ragged) > kMaxGrid / 8 / a->q_heads ||
         ue5m3::attention_items(a->k_tokens, a->sequences, ragged) > kMaxGrid / 8 / a->kv_heads ||
-        (a->q_tokens / 64 + 2) * (a->q_heads / a->kv_heads) > 0x7FFFFFFF)
+        (a->q_tokens / 32 + 2) * (a->q_heads / a->kv_heads) > 0x7FFFFFFF)
         return UE5M3_ESHAPE;
     if (a->q_tokens > 0 && (a->q == nullptr || a->o == nullptr)) return UE5M3_EINVAL;
     if (a->k_tokens > 0 && (a->k == nullptr || a->v == nullptr)) return UE5M3_EINVAL;

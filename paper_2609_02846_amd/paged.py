@@ -5,6 +5,7 @@ import array
 import ctypes
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import _check, _numel, _stream, load_library
 from .operators import recorded
@@ -40,6 +41,7 @@ def copy_pages(cache, src, dst, dim=0):
     numbers = [(ctypes.c_int32 * len(a)).from_buffer(a) if len(a) else None for a in (src, dst)]
     _check(load_library().ue5m3_copy_pages(cache.data_ptr(), _numel(cache.shape[:dim]), pages * page, pages, page, *numbers,
                                            len(src), _stream()), "ue5m3_copy_pages")
+    increment_version(cache)                         # (autograd finds out where it has saved it)
 
 
 class PagedCache:

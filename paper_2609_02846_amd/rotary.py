@@ -12,6 +12,7 @@ import math
 
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from . import PagesC, RopeC, _check, _numel, _ptr, _stream, load_library
 from .operators import _TYPES, recorded
@@ -115,21 +116,40 @@ def _vector(t, name, dtypes, n):
     return t
 
 
+@functools.lru_cache(maxsize=1024)
+def _template(q_shape, q_layout, k_shape, k_layout, dtype, wt, pairs, norm, interleaved):
+    """A RopeC without its addresses, eps and amplitude, as bytes: sizes, types, strides, and
+    dense outputs (an append of one token 18.5 us, with all fields set in each call 19.9)."""
+    dim, q_heads, kv_heads = k_shape[-1], q_shape[-2] if q_shape is not None else 0, k_shape[-2]
+    _, q_token, q_head = q_layout if q_layout is not None else (0, 0, 0)
+    tokens, k_token, k_head = k_layout
+    return bytes(RopeC(tokens, q_heads, kv_heads, dim, pairs, _TYPES[dtype], _TYPES[wt], norm, interleaved, 0.0, 1.0, None, None,
+                       q_token, q_head, k_token, k_head, None, None, None, max(int(k_shape[-3]), 1), None, None, None,
+                       q_heads * dim, dim, kv_heads * dim, dim))
+
+
 def _arguments(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude):
-    """A RopeC of all but the outputs, and the tensors that it points to."""
-    qr, tokens, q_token, q_head = head_rows(q, "q") if q is not None else (None, None, 0, 0)
-    kr, k_tokens, k_token, k_head = head_rows(k, "k")
-    lead, dim = k.shape[:-2], k.shape[-1]
-    if q is not None and (q.shape[:-2] != lead or q.shape[-1] != dim or q.dtype != k.dtype):
-        raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} must have the same tokens, head size and type")
+    """A RopeC of all but the outputs' addresses, and the tensors that it points to."""
+    kr, *k_layout = head_rows(k, "k")
+    shape, dtype = k.shape, k.dtype
+    lead, dim = shape[:-2], shape[-1]
+    qr = q_shape = q_layout = None
+    if q is not None:
+        qr, *q_layout = head_rows(q, "q")
+        q_shape = q.shape
+        if q_shape[:-2] != lead or q_shape[-1] != dim or q.dtype != dtype:
+            raise ValueError(f"q {tuple(q_shape)} and k {tuple(shape)} must have the same tokens, head size and type")
+        q_layout = tuple(q_layout)
     if not 1 <= dim <= 256:
         raise ValueError("heads have 1 to 256 elements")
-    norm = eps is not None
-    if not norm and (q_weight is not None or k_weight is not None):
-        raise ValueError("weights belong to the norm: pass eps")
-    wt = next((w.dtype for w in (q_weight, k_weight) if w is not None), k.dtype)
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        _vector(w, name, (wt,) if wt in (k.dtype, torch.float32) else (k.dtype, torch.float32), dim)
+    norm, wt = eps is not None, dtype
+    if q_weight is not None or k_weight is not None:
+        if not norm:
+            raise ValueError("weights belong to the norm: pass eps")
+        wt = (k_weight if q_weight is None else q_weight).dtype
+        types = (wt,) if wt in (dtype, torch.float32) else (dtype, torch.float32)
+        _vector(q_weight, "q_weight", types, dim)
+        _vector(k_weight, "k_weight", types, dim)
     pairs = 0
     if freqs is not None:
         pairs = freqs.numel()
@@ -146,23 +166,18 @@ def _arguments(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amp
                 positions = positions.to(torch.int64).expand(lead).contiguous()
     else:
         positions = None
-    args = RopeC(k_tokens, q.shape[-2] if q is not None else 0, k.shape[-2], dim, pairs, _TYPES[k.dtype], _TYPES[wt],
-                 int(norm), int(bool(interleaved)), float(eps) if norm else 0.0, float(amplitude), _ptr(qr), _ptr(kr),
-                 q_token, q_head, k_token, k_head, _ptr(q_weight), _ptr(k_weight), _ptr(positions), max(int(lead[-1]), 1),
-                 _ptr(freqs))
+    args = RopeC.from_buffer_copy(_template(q_shape, q_layout, shape, tuple(k_layout), dtype, wt, pairs, int(norm),
+                                            int(bool(interleaved))))
+    args.eps, args.amplitude = float(eps) if norm else 0.0, float(amplitude)
+    args.q, args.k, args.q_weight, args.k_weight = _ptr(qr), _ptr(kr), _ptr(q_weight), _ptr(k_weight)
+    args.positions, args.freqs = _ptr(positions), _ptr(freqs)
     return args, (qr, kr, positions)
-
-
-def _dense(args, q_out, k_out):
-    dim = args.dim
-    args.q_out, args.q_out_token, args.q_out_head = _ptr(q_out), args.q_heads * dim, dim
-    args.k_out, args.k_out_token, args.k_out_head = _ptr(k_out), args.kv_heads * dim, dim
 
 
 def _forward(q, k, *rest):
     args, kept = _arguments(q, k, *rest)
     q_out, k_out = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
-    _dense(args, q_out, k_out)
+    args.q_out, args.k_out = q_out.data_ptr(), k_out.data_ptr()
     _check(load_library().ue5m3_qk_norm_rope(args, _stream()), "ue5m3_qk_norm_rope")
     return q_out, k_out, kept
 
@@ -192,7 +207,7 @@ class _RopeFn(torch.autograd.Function):
         new = lambda t, need: torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None  # noqa: E731
         dq, dk = new(gq, need_q), new(gk, need_k)
         dqw, dkw = new(q_weight, need_qw and q_weight is not None), new(k_weight, need_kw and k_weight is not None)
-        _dense(args, dq, dk)
+        args.q_out, args.k_out = _ptr(dq), _ptr(dk)
         lib, scratch = load_library(), None
         if dqw is not None or dkw is not None:
             n = lib.ue5m3_qk_norm_rope_grad_scratch(args.tokens, args.q_heads + args.kv_heads, args.dim)
@@ -214,7 +229,7 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, positions=None, freqs=None,
     together.  ``positions``: integers [..., L], broadcast over leading dimensions
     (None: 0 .. L - 1 in each).  The weights' gradients are summed in fp32 in a fixed
     order.  Returns new dense tensors (q, k)."""
-    if recorded(q, k, q_weight, k_weight):
+    if recorded(q, k, q_weight, k_weight, freqs):
         return _RopeFn.apply(q, k, q_weight, k_weight, positions, freqs, eps, bool(interleaved), float(amplitude))
     return _forward(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude)[:2]
 
@@ -251,7 +266,7 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None, k_weigh
     ue5m3_qk_norm_rope_append).  A slot below 0 or past the cache writes nothing.
     ``q`` may be None (keys that are ready: with eps=None and no freqs they are
     copied); then None is returned."""
-    if recorded(q, k, v, q_weight, k_weight):
+    if recorded(q, k, v, q_weight, k_weight, freqs, k_cache, v_cache):
         raise RuntimeError("qk_norm_rope_append has no gradients: call it under torch.no_grad()")
     args, kept = _arguments(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amplitude)
     vr, tokens, v_token, v_head = head_rows(v, "v")
@@ -264,7 +279,8 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None, k_weigh
     if slots.dtype != torch.int64 or slots.numel() != tokens or not slots.is_contiguous():
         raise ValueError(f"slots must be {tokens} contiguous int64 numbers")
     q_out = None if q is None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _dense(args, q_out, None)
+    args.q_out = _ptr(q_out)
     _check(load_library().ue5m3_qk_norm_rope_append(args, vr.data_ptr(), v_token, v_head, cache, slots.data_ptr(), _stream()),
            "ue5m3_qk_norm_rope_append")
+    increment_version((k_cache, v_cache))            # (autograd finds out where it has saved them)
     return q_out

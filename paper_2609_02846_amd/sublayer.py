@@ -128,6 +128,13 @@ class PreNormAttention(torch.nn.Module):
         freqs, self.amplitude = rotary_frequencies(head_dim, device=device) if rotary is None else rotary
         self.register_buffer("freqs", freqs, persistent=False)
 
+    def _apply(self, fn, recurse=True):
+        freqs = self.freqs
+        super()._apply(fn, recurse)
+        if self.freqs.dtype != torch.float32:        # (moved with the module, not cast with it)
+            self.freqs = freqs.to(self.freqs.device)
+        return self
+
     def _rotary(self, positions):
         return self.q_weight, self.k_weight, positions, self.freqs, self.qk_eps, False, self.amplitude
 
