@@ -101,7 +101,7 @@ ue5m3_status_t attention_args(const ue5m3_attention_t* a) {
 // Whether the sizes that scratch memory goes by are such.
 bool sizes_ok(const ue5m3_attention_t* a) {
     return a != nullptr && a->q_tokens >= 0 && a->q_tokens <= kMaxTokens && a->k_tokens >= 0 && a->k_tokens <= kMaxTokens &&
-           a->sequences >= 1 && a->q_heads >= 1 && a->q_heads <= kMaxHeads && a->kv_heads >= 1 && a->kv_heads <= a->q_heads &&
+           a->sequences >= 1 && a->sequences <= kMaxTokens && a->q_heads >= 1 && a->q_heads <= kMaxHeads && a->kv_heads >= 1 && a->kv_heads <= a->q_heads &&
            a->dim >= 1 && a->dim <= 128 && a->window >= 0 && a->sinks >= 0;
 }
 

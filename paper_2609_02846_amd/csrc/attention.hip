@@ -527,12 +527,14 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
 }
 
 // Of the gradient's scratch memory: delta and the references [2][heads][tokens], then
-// the parts of dK and dV [parts][2][tokens][kv_heads][dim].
+// the parts of dK and dV [parts][2][tokens][kv_heads][dim], then those of the sinks from
+// the rows far from them [far][2][sequences][sinks][kv_heads][dim].
 __host__ __device__ inline int64_t dkv_floats(const ue5m3_attention_t& a) { return a.k_tokens * a.kv_heads * a.dim; }
 __host__ __device__ inline int64_t delta_floats(const ue5m3_attention_t& a) { return (2 * a.q_heads * a.q_tokens + 3) / 4 * 4; }
 __device__ __forceinline__ float* dkv_parts(const ue5m3_attention_t& a, const ue5m3_attention_grad_t& g) {
     return (float*)g.scratch + delta_floats(a);
 }
+__host__ __device__ inline int64_t far_floats(const ue5m3_attention_t& a) { return a.sequences * a.sinks * a.kv_heads * a.dim; }
 
 // dK and dV: a workgroup takes 128 keys of a key-value head, 32 a wave, and walks
 // through the queries that see them, 32 at a time, of each query head that shares
@@ -546,9 +548,12 @@ __device__ __forceinline__ float* dkv_parts(const ue5m3_attention_t& a, const ue
 // Bound: the products, 4 of 2 pairs x heads x dim operations, and LDS, which holds Q and
 // dO for two reads each: those 1.10 TF take 1230 us (893 TFLOP/s), the matrix pipe works
 // in 43% of the cycles, half of the waves' others go on waiting for reads of LDS.
+//
+// Under a window the first tile of a sequence has all rows to visit where the others have
+// the window's: the rows that see its sinks only are cut into `far` parts of their own.
 template <typename T, int DT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items,
-                                                                       int parts) {
+                                                                       int parts, int far) {
     constexpr int kQ = 32, kTile = kQ * DT * 2, kB = DT / 32, kS = DT / 16;
     __shared__ __attribute__((aligned(16))) uint8_t sQ[2 * kTile];
     __shared__ __attribute__((aligned(16))) uint8_t sD[2 * kTile];
@@ -556,17 +561,23 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
     __shared__ __attribute__((aligned(16))) float sR[2 * 64];        // delta of the tile's rows, then their references
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
     const int kv = blockIdx.x % a.kv_heads, group = a.q_heads / a.kv_heads;
-    const int part = blockIdx.x / a.kv_heads % parts, item = blockIdx.x / (a.kv_heads * parts);
-    const Span w = find_span<kRows, true, false>(item, a.sequences, a.q_starts, a.k_starts, a.q_tokens, a.k_tokens);
+    const int far_groups = far * (int)a.sequences, id = (int)(blockIdx.x / a.kv_heads) - far_groups;
+    const bool is_far = id < 0, staged = parts > 1 || far > 0;
+    const int shares = is_far ? far : parts, at_id = is_far ? id + far_groups : id;
+    const int part = at_id % shares, item = at_id / shares;      // (of the far ones the sequence)
+    const Span w = is_far ? span_of(item, a.sequences, a.q_starts, a.k_starts, a.q_tokens, a.k_tokens)
+                          : find_span<kRows, true, false>(item, a.sequences, a.q_starts, a.k_starts, a.q_tokens, a.k_tokens);
+    if (is_far && w.keys == 0) return;
     float* const delta = (float*)g.scratch;
-    float* const part_dk = dkv_parts(a, g) + (int64_t)part * 2 * dkv_floats(a) + (int64_t)kv * a.dim;
-    float* const part_dv = part_dk + dkv_floats(a);
+    float* part_dk = dkv_parts(a, g) + (int64_t)kv * a.dim;
+    part_dk += is_far ? parts * 2 * dkv_floats(a) + part * 2 * far_floats(a) : part * 2 * dkv_floats(a);
+    float* const part_dv = part_dk + (is_far ? far_floats(a) : dkv_floats(a));
     T* const dk_head = (T*)g.dk + kv * g.dk_head;
     T* const dv_head = (T*)g.dv + kv * g.dv_head;
     const int64_t token = (int64_t)a.kv_heads * a.dim;   // of the parts
     if (w.tile < 0) {
         const int extras = items - (item - w.extra);
-        if (parts > 1) {
+        if (staged) {
             clear_outside(part_dk, token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, (float*)nullptr);
             clear_outside(part_dv, token, a.k_starts, a.sequences, a.k_tokens, a.dim, w.extra, extras, (float*)nullptr);
         } else {
@@ -596,11 +607,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
     const int end = min(c0 + kRows, w.keys) - 1;
     int from = 0, to = w.rows;
     if (sees.causal) from = max(0, c0 - off);
-    if (limited && c0 >= sees.sinks) to = (int)min((int64_t)to, (int64_t)end + sees.window - off);
+    if (limited && (c0 >= sees.sinks || far > 0)) to = (int)min((int64_t)to, (int64_t)end + sees.window - off);
     from = from / kQ;
+    if (is_far) from = (max(to, 0) + kQ - 1) / kQ, to = w.rows;
     // of all heads' tiles, one after the other, this part's share
     const int per = max(0, (to + kQ - 1) / kQ - from);
-    const int i0 = (int)((int64_t)per * group * part / parts), n = (int)((int64_t)per * group * (part + 1) / parts) - i0;
+    const int i0 = (int)((int64_t)per * group * part / shares), n = (int)((int64_t)per * group * (part + 1) / shares) - i0;
 
     const uint32_t ldsQ = lds_addr(sQ), ldsD = lds_addr(sD), ldsR = lds_addr(sR);
     if (n > 0) {                                     // (the first turn waits for them)
@@ -770,22 +782,44 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
         turn(std::integral_constant<int, 1>{});
         --left;
     }
-    if (key >= w.keys) return;
-    if (parts > 1) {
+    if (key >= w.keys || (is_far && key >= sees.sinks)) return;
+    if (staged) {
+        const int64_t row = is_far ? item * a.sinks + key : at;
 #pragma unroll
         for (int b = 0; b < kB; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int d = 32 * b + 8 * e + 4 * h;
                 if (d < a.dim) {
-                    *(f32x4*)(part_dk + at * token + d) = f32x4{dk[b][4 * e], dk[b][4 * e + 1], dk[b][4 * e + 2], dk[b][4 * e + 3]};
-                    *(f32x4*)(part_dv + at * token + d) = f32x4{dv[b][4 * e], dv[b][4 * e + 1], dv[b][4 * e + 2], dv[b][4 * e + 3]};
+                    *(f32x4*)(part_dk + row * token + d) = f32x4{dk[b][4 * e], dk[b][4 * e + 1], dk[b][4 * e + 2], dk[b][4 * e + 3]};
+                    *(f32x4*)(part_dv + row * token + d) = f32x4{dv[b][4 * e], dv[b][4 * e + 1], dv[b][4 * e + 2], dv[b][4 * e + 3]};
                 }
             }
     } else {
         store_column<T, DT>(dk_head + at * g.dk_token, dk, a.scale, a.dim);
         store_column<T, DT>(dv_head + at * g.dv_token, dv, 1.0f, a.dim);
     }
+}
+
+// The sinks' parts from the rows far from them, in their order, added to the first part of
+// the rest; a thread four elements of both.
+__global__ __launch_bounds__(kAttnThreads) void attention_sink_sum_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int parts,
+                                                                         int far) {
+    const int64_t n = far_floats(a), i = ((int64_t)blockIdx.x * kAttnThreads + threadIdx.x) * 4;
+    if (i >= n) return;
+    const int64_t token = (int64_t)a.kv_heads * a.dim, row = i / token, seq = row / a.sinks, key = row - seq * a.sinks;
+    const Span w = span_of(seq, a.sequences, a.q_starts, a.k_starts, a.q_tokens, a.k_tokens);
+    if (key >= w.keys) return;
+    const float* p = dkv_parts(a, g) + parts * 2 * dkv_floats(a) + i;
+    float* const to = dkv_parts(a, g) + (w.k0 + key) * token + i % token;
+    f32x4 dk = *(const f32x4*)to, dv = *(const f32x4*)(to + dkv_floats(a));
+#pragma unroll 8
+    for (int k = 0; k < far; ++k, p += 2 * n) {
+        dk += *(const f32x4*)p;
+        dv += *(const f32x4*)(p + n);
+    }
+    *(f32x4*)to = dk;
+    *(f32x4*)(to + dkv_floats(a)) = dv;
 }
 
 // dK and dV from their parts, in their order; a thread four elements of both.
@@ -866,15 +900,32 @@ int dkv_parts_of(const ue5m3_attention_t& a) {
     return (int)std::max<int64_t>(1, std::min<int64_t>({8, (4 * kCus + work - 1) / work, turns / 16}));
 }
 
+// Parts that the rows are cut into that see of a sequence's first tile the sinks only (0:
+// they stay with the others): of the longest that a sequence can be, about as many turns
+// each as a part of the other tiles has, two for each sequence at least, and no more of
+// them than memory for two parts of all keys holds (8192 tokens, window 1024, 4 sinks, 32
+// heads of 128, 8 of keys, forward and gradients: 1550 us with them among the others, 899
+// apart; 16 heads of 64 494 and 303).
+int far_parts_of(const ue5m3_attention_t& a, int parts) {
+    if (!a.causal || a.window == 0 || a.sinks == 0 || a.sinks > kRows || a.sequences * a.kv_heads >= 1 << 21) return 0;
+    const int64_t n = a.q_starts != nullptr ? 1 : a.sequences, group = a.q_heads / a.kv_heads;
+    const int64_t keys = a.k_tokens / n, window = std::min(a.window, keys), rows = std::min(a.q_tokens / n, keys - window - kRows);
+    if (rows <= 0) return 0;
+    const int64_t turns = (window + kRows) / 32 * group / parts, want = rows / 32 * group / std::max<int64_t>(turns, 16);
+    const int64_t room = 2 * a.k_tokens / (a.sequences * a.sinks);
+    const int64_t far = std::min<int64_t>({want, room, 64, std::max<int64_t>(2, 4 * kCus / (a.sequences * a.kv_heads))});
+    return far < 2 ? 0 : (int)far;
+}
+
 int64_t attention_grad_scratch(const ue5m3_attention_t& a) {
-    const int parts = dkv_parts_of(a);
-    return (delta_floats(a) + (parts > 1 ? 2 * parts * dkv_floats(a) : 0)) * 4;
+    const int parts = dkv_parts_of(a), far = far_parts_of(a, parts);
+    return (delta_floats(a) + (parts > 1 || far > 0 ? 2 * parts * dkv_floats(a) + 2 * far * far_floats(a) : 0)) * 4;
 }
 
 hipError_t launch_attention_grad(const ue5m3_attention_t& a, const ue5m3_attention_grad_t& g, hipStream_t s) {
     const int64_t rows = attention_items(a.q_tokens, a.sequences, a.q_starts != nullptr);
     const int64_t keys = attention_items(a.k_tokens, a.sequences, a.k_starts != nullptr);
-    const int parts = dkv_parts_of(a);
+    const int parts = dkv_parts_of(a), far = far_parts_of(a, parts);
     return with_head((DType)a.type, a.dim, [&](auto* t, auto d) {
         using T = std::remove_pointer_t<decltype(t)>;
         constexpr int DT = decltype(d)::value;
@@ -885,10 +936,16 @@ hipError_t launch_attention_grad(const ue5m3_attention_t& a, const ue5m3_attenti
             e = hipGetLastError();
         }
         if (e != hipSuccess || g.dk == nullptr || a.k_tokens == 0) return e;
-        hipLaunchKernelGGL((attention_dkv_kernel<T, DT>), dim3((unsigned)(keys * parts * a.kv_heads)), dim3(kAttnThreads), 0,
-                           s, a, g, (int)keys, parts);
+        hipLaunchKernelGGL((attention_dkv_kernel<T, DT>), dim3((unsigned)((keys * parts + far * a.sequences) * a.kv_heads)),
+                           dim3(kAttnThreads), 0, s, a, g, (int)keys, parts, far);
         e = hipGetLastError();
-        if (e != hipSuccess || parts == 1) return e;
+        if (e == hipSuccess && far > 0) {
+            const int64_t threads = far_floats(a) / 4;
+            hipLaunchKernelGGL(attention_sink_sum_kernel, dim3((unsigned)((threads + kAttnThreads - 1) / kAttnThreads)),
+                               dim3(kAttnThreads), 0, s, a, g, parts, far);
+            e = hipGetLastError();
+        }
+        if (e != hipSuccess || (parts == 1 && far == 0)) return e;
         const int64_t threads = (dkv_floats(a) + 3) / 4;
         hipLaunchKernelGGL((attention_dkv_sum_kernel<T>), dim3((unsigned)((threads + kAttnThreads - 1) / kAttnThreads)),
                            dim3(kAttnThreads), 0, s, a, g, parts);

@@ -202,6 +202,17 @@ __device__ __forceinline__ void bounds(const int32_t* starts, int64_t i, int64_t
     to = min(max((int64_t)starts[i + 1], from), tokens);
 }
 
+// Sequence `seq`, at its first tile.
+__device__ __forceinline__ Span span_of(int64_t seq, int64_t n, const int32_t* q_starts, const int32_t* k_starts, int64_t q_tokens,
+                                        int64_t k_tokens) {
+    int64_t q0 = seq * (q_tokens / n), k0 = seq * (k_tokens / n), q1 = q0 + q_tokens / n, k1 = k0 + k_tokens / n;
+    if (q_starts != nullptr) {
+        bounds(q_starts, seq, q_tokens, q0, q1);
+        bounds(k_starts, seq, k_tokens, k0, k1);
+    }
+    return Span{q0, k0, (int)(q1 - q0), (int)(k1 - k0), 0, 0};
+}
+
 // Work item `id` of all sequences' tiles of TILE rows, of queries or (KEYS) of
 // keys; with DOWN the last tiles first.  All lanes of a wave call it.
 template <int TILE, bool KEYS, bool DOWN>
