@@ -7,7 +7,7 @@ from torch.autograd.function import once_differentiable
 
 from . import AttentionC, AttentionGradC, PagedAttentionC, _check, _numel, _ptr, _stream, load_library
 from .operators import _TYPES, recorded
-from .rotary import _on_device, cache_arguments, head_rows
+from .rotary import _on_device, cache_arguments, dense_like, head_rows
 
 _HALF = (torch.bfloat16, torch.float16)
 
@@ -70,12 +70,12 @@ def attention_forward(q, k, v, q_starts=None, k_starts=None, scale=None, causal=
     """``attention`` without gradients; with ``lse`` (o, lse): the fp32 logarithms of
     the rows' sums [heads, tokens]."""
     args, kept = _arguments(q, k, v, q_starts, k_starts, scale, causal, window, sinks)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    o = dense_like(q)
     sums = torch.empty((args.q_heads, args.q_tokens), dtype=torch.float32, device=q.device) if lse else None
     args.o, args.lse = o.data_ptr(), _ptr(sums)
     rest = None
     if _rest:
-        rest = torch.empty_like(o)
+        rest = dense_like(o)
         args.o_rest = rest.data_ptr()
     lib = load_library()
     n = lib.ue5m3_attention_scratch(args)
@@ -102,9 +102,8 @@ class _AttentionFn(torch.autograd.Function):
         do = do.contiguous()
         if do.data_ptr() % 16:
             do = do.clone()
-        new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
-        dq = new(q) if need_q else None
-        dk, dv = (new(k), new(v)) if need_k or need_v else (None, None)
+        dq = dense_like(q) if need_q else None
+        dk, dv = (dense_like(k), dense_like(v)) if need_k or need_v else (None, None)
         lib = load_library()
         scratch = torch.empty(lib.ue5m3_attention_grad_scratch(args), dtype=torch.uint8, device=lse.device)
         qs, ks, d = q.shape[-2] * q.shape[-1], k.shape[-2] * k.shape[-1], q.shape[-1]
@@ -162,7 +161,7 @@ def paged_attention(q, k_cache, v_cache, table, lengths, scale=None, window=0, s
     width, window, sinks = table.shape[1], int(window), int(sinks)
     _heads(q.shape[1], k_cache.shape[2], q.shape[2], window, sinks)
     lib = load_library()
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    o = dense_like(q)
     n = lib.ue5m3_paged_attention_scratch(rows, q.shape[1], k_cache.shape[2], q.shape[2], width * cache.page_size, window, sinks)
     scratch = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     args = PagedAttentionC(rows, q.shape[1], k_cache.shape[2], q.shape[2], _TYPES[q.dtype],

@@ -107,6 +107,11 @@ def head_rows(t, name, dtypes=_TYPES, dense=False):
     return (t, *layout)
 
 
+def dense_like(t):
+    """An uninitialised dense tensor of t's shape and type (1.2 us; torch.empty of them 2.3)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _vector(t, name, dtypes, n):
     if t is None:
         return None
@@ -176,7 +181,7 @@ def _arguments(q, k, q_weight, k_weight, positions, freqs, eps, interleaved, amp
 
 def _forward(q, k, *rest):
     args, kept = _arguments(q, k, *rest)
-    q_out, k_out = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    q_out, k_out = dense_like(q), dense_like(k)
     args.q_out, args.k_out = q_out.data_ptr(), k_out.data_ptr()
     _check(load_library().ue5m3_qk_norm_rope(args, _stream()), "ue5m3_qk_norm_rope")
     return q_out, k_out, kept
@@ -204,7 +209,7 @@ class _RopeFn(torch.autograd.Function):
         # (without the norm the inputs do not matter: the gradients stand in for them)
         args, kept = _arguments(gq if q is None else q, gk if k is None else k, q_weight, k_weight, positions, freqs, *ctx.rest)
         need_q, need_k, need_qw, need_kw = ctx.needs_input_grad[:4]
-        new = lambda t, need: torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None  # noqa: E731
+        new = lambda t, need: dense_like(t) if need else None  # noqa: E731
         dq, dk = new(gq, need_q), new(gk, need_k)
         dqw, dkw = new(q_weight, need_qw and q_weight is not None), new(k_weight, need_kw and k_weight is not None)
         args.q_out, args.k_out = _ptr(dq), _ptr(dk)
@@ -278,7 +283,7 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None, k_weigh
     _on_device(slots, "slots")
     if slots.dtype != torch.int64 or slots.numel() != tokens or not slots.is_contiguous():
         raise ValueError(f"slots must be {tokens} contiguous int64 numbers")
-    q_out = None if q is None else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    q_out = None if q is None else dense_like(q)
     args.q_out = _ptr(q_out)
     _check(load_library().ue5m3_qk_norm_rope_append(args, vr.data_ptr(), v_token, v_head, cache, slots.data_ptr(), _stream()),
            "ue5m3_qk_norm_rope_append")
