@@ -770,7 +770,8 @@ ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, void* scratch, hip
  * dk = scale dS^T q, dv = P^T d_o, the last two summed over the query heads that share
  * a key-value head, in a fixed order.  `args` as of the forward call, with its o,
  * o_rest and lse; `scratch` has ue5m3_attention_grad_scratch(args) bytes.  dq, or dk and dv
- * together, may be null.  16-byte alignment and strides as for q, k and v.
+ * together, may be null.  16-byte alignment and strides as for q, k and v.  EINVAL also: a
+ * type that is not bf16 (of fp16, dS of a mean over tokens is below the normal numbers).
  */
 typedef struct {
     const void* d_o;

@@ -204,7 +204,7 @@ ue5m3_status_t ue5m3_attention_grad(const ue5m3_attention_t* args, const ue5m3_a
                                     hipStream_t stream) {
     const ue5m3_status_t st = attention_args(args);
     if (st != UE5M3_OK) return st;
-    if (grad == nullptr || (grad->dk == nullptr) != (grad->dv == nullptr)) return UE5M3_EINVAL;
+    if (grad == nullptr || (grad->dk == nullptr) != (grad->dv == nullptr) || args->type != UE5M3_BF16) return UE5M3_EINVAL;
     const ue5m3_attention_grad_t& g = *grad;
     if (ue5m3::attention_grad_scratch(*args) > 0 && g.scratch == nullptr) return UE5M3_EINVAL;
     if (args->q_tokens > 0 && (g.d_o == nullptr || args->lse == nullptr || args->o_rest == nullptr)) return UE5M3_EINVAL;

@@ -842,12 +842,13 @@ __global__ __launch_bounds__(kAttnThreads) void attention_dkv_sum_kernel(ue5m3_a
 }
 
 // Calls f(null pointer of the type, the padded head size).
+template <typename T, typename F>
+hipError_t with_size(T* t, int dim, F&& f) {
+    return dim <= 64 ? f(t, std::integral_constant<int, 64>{}) : f(t, std::integral_constant<int, 128>{});
+}
 template <typename F>
 hipError_t with_head(DType type, int dim, F&& f) {
-    auto sized = [&](auto* t) {
-        return dim <= 64 ? f(t, std::integral_constant<int, 64>{}) : f(t, std::integral_constant<int, 128>{});
-    };
-    return type == DType::BF16 ? sized((bf16*)nullptr) : sized((f16*)nullptr);
+    return type == DType::BF16 ? with_size((bf16*)nullptr, dim, f) : with_size((f16*)nullptr, dim, f);
 }
 
 }  // namespace
@@ -926,7 +927,7 @@ hipError_t launch_attention_grad(const ue5m3_attention_t& a, const ue5m3_attenti
     const int64_t rows = attention_items(a.q_tokens, a.sequences, a.q_starts != nullptr);
     const int64_t keys = attention_items(a.k_tokens, a.sequences, a.k_starts != nullptr);
     const int parts = dkv_parts_of(a), far = far_parts_of(a, parts);
-    return with_head((DType)a.type, a.dim, [&](auto* t, auto d) {
+    return with_size((bf16*)nullptr, a.dim, [&](auto* t, auto d) {
         using T = std::remove_pointer_t<decltype(t)>;
         constexpr int DT = decltype(d)::value;
         hipError_t e = hipSuccess;

@@ -6,7 +6,8 @@ import pytest
 import torch
 from torch.autograd import forward_ad
 
-from paper_2609_02846_amd.attention import attention, attention_forward, paged_attention
+from paper_2609_02846_amd import AttentionC, AttentionGradC, load_library
+from paper_2609_02846_amd.attention import attention, paged_attention
 from paper_2609_02846_amd.paged import copy_pages
 from paper_2609_02846_amd.rotary import qk_norm_rope, qk_norm_rope_append
 from paper_2609_02846_amd.sublayer import PreNormAttention
@@ -62,6 +63,16 @@ def test_serving_calls_drop_no_gradient(what):
 def test_frequencies_have_no_gradient():
     with pytest.raises((ValueError, RuntimeError)):
         qk_norm_rope(H, H, freqs=F.clone().requires_grad_())
+
+
+def test_gradients_are_of_bf16():
+    """The library's own entry refuses fp16 as the binding does, before any pointer."""
+    lib = load_library()
+    sizes = dict(q_tokens=0, k_tokens=0, sequences=1, q_heads=4, kv_heads=2, dim=64, causal=1, scale=0.1, q_token=256, q_head=64,
+                 k_token=128, k_head=64, v_token=128, v_head=64)
+    assert lib.ue5m3_attention_grad(AttentionC(type=0, **sizes), AttentionGradC(), None) == 0
+    assert lib.ue5m3_attention_grad(AttentionC(type=1, **sizes), AttentionGradC(), None) == 1
+    assert lib.ue5m3_attention(AttentionC(type=1, **sizes), None, None) == 0
 
 
 def test_the_branch_keeps_its_frequencies():
