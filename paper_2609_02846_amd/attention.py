@@ -123,8 +123,8 @@ def attention(q, k, v, q_starts=None, k_starts=None, scale=None, causal=True, wi
     keys up to its own position; of these, with ``window`` > 0, the last ``window`` ones
     and the first ``sinks``.  A query that sees nothing gives zeros, as do tokens of no
     sequence.  What a query does not see may be anything (for gradients all of a sequence
-    has to be finite).  ``scale``: of the scores (None: dim^-1/2).  See ue5m3_attention.  The same call gives the same
-    bits, gradients included."""
+    has to be finite).  ``scale``: of the scores (None: dim^-1/2).  The same call gives the
+    same bits, gradients included.  See ue5m3_attention."""
     if recorded(q, k, v):
         if isinstance(q, torch.Tensor) and q.dtype == torch.float16:
             raise NotImplementedError("attention in fp16 has no gradients")

@@ -267,7 +267,7 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None, k_weigh
     """The serving form of ``qk_norm_rope``: returns the queries, and writes the keys,
     normed and rotated, and the values ``v`` into a cache (``k_cache``, ``v_cache``
     [pages, page_size, kv_heads, dim], any strides with a head's elements together), token
-    t at ``slots``[t] (int64) = page * page_size + place (see
+    t at ``slots``[t] (int64) = page * page_size + place, no two at one (see
     ue5m3_qk_norm_rope_append).  A slot below 0 or past the cache writes nothing.
     ``q`` may be None (keys that are ready: with eps=None and no freqs they are
     copied); then None is returned."""
