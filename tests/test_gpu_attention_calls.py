@@ -142,6 +142,47 @@ def test_batches_of_nothing():
     assert x.grad.shape == (0, 128) and not m.q_weight.grad.any() and not m.qkv.weight.grad.any()
 
 
+def test_offsets_past_32_bits():
+    """Tokens 8 MB apart: the same bits as of dense ones."""
+    say("far apart")
+    T, step = 600, 1 << 22                           # the last token is 5 GB from the first
+
+    def apart(t):
+        store = torch.empty((T - 1) * step + t[0].numel(), dtype=t.dtype, device="cuda")
+        far = store.as_strided(t.shape, (step, t.shape[2], 1))
+        return far.copy_(t)
+    dense = [rand(1, T, 4, 64), rand(2, T, 2, 64), rand(3, T, 2, 64)]
+    do, f = rand(4, T, 4, 64), rotary_frequencies(64)[0]
+    want = got = None
+    for tensors in (dense, [apart(t) for t in dense]):
+        q, k, v = (t.detach().requires_grad_() for t in tensors)
+        a, b = qk_norm_rope(q, k, freqs=f)
+        o = attention(q, k, v, window=100, sinks=3)
+        got = [a, b, o, *torch.autograd.grad(o, (q, k, v), do), *torch.autograd.grad((a, b), (q, k), (do, dense[1]))]
+        if want is None:
+            want = got
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_another_stream():
+    """Forward and backward pass on a stream of their own, its memory used again at once."""
+    say("another stream")
+    x = [rand(i, 400, 4, 64).requires_grad_() for i in range(3)]
+    do = rand(9, 400, 4, 64)
+
+    def step():
+        a, b = qk_norm_rope(x[0], x[1], freqs=f)
+        return torch.autograd.grad(attention(a, b, x[2], window=64, sinks=2), x, do)
+    f = rotary_frequencies(64)[0]
+    want = step()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = [step() for _ in range(10)]
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
+
+
 def test_a_branch_cast_with_its_model():
     """The rotation is that of the frequencies in 32 bits."""
     say("cast")
