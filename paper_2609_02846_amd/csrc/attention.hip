@@ -547,12 +547,15 @@ __host__ __device__ inline int64_t far_floats(const ue5m3_attention_t& a) { retu
 //
 // Bound: the products, 4 of 2 pairs x heads x dim operations, and LDS, which holds Q and
 // dO for two reads each: those 1.10 TF take 1230 us (893 TFLOP/s), the matrix pipe works
-// in 43% of the cycles, half of the waves' others go on waiting for reads of LDS.
+// in 43% of the cycles, half of the waves' others go on waiting for reads of LDS.  With heads
+// of 64 three workgroups fit a CU, which is worth more than products ordered between the
+// exponentials by hand, for which there are registers with two only (packed sequences of
+// 8192 tokens, window 1024, 4 sinks: 108 us against 119).
 //
 // Under a window the first tile of a sequence has all rows to visit where the others have
 // the window's: the rows that see its sinks only are cut into `far` parts of their own.
 template <typename T, int DT>
-__global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items,
+__global__ __launch_bounds__(kAttnThreads, DT == 64 ? 3 : 2) void attention_dkv_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items,
                                                                        int parts, int far) {
     constexpr int kQ = 32, kTile = kQ * DT * 2, kB = DT / 32, kS = DT / 16;
     __shared__ __attribute__((aligned(16))) uint8_t sQ[2 * kTile];
@@ -673,11 +676,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
     }
     int rb = top - skip, left = n;
     // One tile, in a buffer that is known when this is compiled, so that the addresses
-    // of all reads are a few registers and constants.  With heads of 64 dP's products run
-    // between the exponentials, dV's between what makes dS of them; heads of 128 have no
-    // registers for dP that early.
-    constexpr bool EARLY = DT == 64;
-    auto work = [&](auto buffer, auto masked, int r0) __attribute__((always_inline)) {
+    // of all reads are a few registers and constants.
+    auto work = [&](auto buffer, bool masked, int r0) __attribute__((always_inline)) {
         constexpr int B = decltype(buffer)::value;
         const uint8_t *tq = sQ + B * kTile, *td = sD + B * kTile, *tv = sV + wave * (32 * DT * 2);
         const float* tr = sR + B * 64 + 4 * h;
@@ -687,12 +687,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
         for (int e = 0; e < 16; ++e) s[e] = t[e] = 0.0f;
 #pragma unroll
         for (int x = 0; x < kS; ++x) s = product32<T>(read_along<DT>(tq, 0, x, lane), k[x], s);
-        auto dp = [&]() {
-#pragma unroll
-            for (int x = 0; x < kS; ++x)
-                t = product32<T>(read_along<DT>(td, 0, x, lane), read_along<DT>(tv, 0, x, lane), t);
-        };
-        if (EARLY) dp();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const f32x4 ref = *(const f32x4*)(tr + 32 + 8 * e);
@@ -714,7 +708,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
 #pragma unroll
             for (int y = 0; y < kB; ++y) dv[y] = product32<T>(read_across<DT>(td, 16 * x, y, lane), pt, dv[y]);
         }
-        if (!EARLY) dp();
+#pragma unroll
+        for (int x = 0; x < kS; ++x) t = product32<T>(read_along<DT>(td, 0, x, lane), read_along<DT>(tv, 0, x, lane), t);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const f32x4 delta = *(const f32x4*)(tr + 8 * e);
@@ -736,33 +731,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
 #pragma unroll
             for (int y = 0; y < kB; ++y) dk[y] = product32<T>(read_across<DT>(tq, 16 * x, y, lane), ds, dk[y]);
         }
-        if (EARLY && !masked) {
-            __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
-#pragma unroll
-            for (int x = 0; x < kS; ++x) {
-                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
-#pragma unroll
-            for (int x = 0; x < kS; ++x) {
-                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgValu, 24 / kS, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgTrans, 16 / kS, 0);
-            }
-#pragma unroll
-            for (int x = 0; x < 2 * kB; ++x) {
-                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgValu, 40 / (2 * kB), 0);
-            }
-#pragma unroll
-            for (int x = 0; x < 2 * kB; ++x) {
-                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
-            }
-        }
     };
     auto turn = [&](auto buffer) __attribute__((always_inline)) {
         wait_loads<0>();
@@ -771,10 +739,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dkv_kernel(ue5m3_at
         const int r0 = rb;
         rb = rb > from * kQ ? rb - kQ : top;
         if (r0 + kQ <= some_lo || r0 >= some_hi) return;
-        const bool all = r0 >= all_lo && r0 + kQ <= all_hi;
-        if (!EARLY) work(buffer, !all, r0);
-        else if (all) work(buffer, std::false_type{}, r0);
-        else work(buffer, std::true_type{}, r0);
+        work(buffer, r0 < all_lo || r0 + kQ > all_hi, r0);
     };
     while (left > 0) {
         turn(std::integral_constant<int, 0>{});
