@@ -16,6 +16,10 @@
 // 8192 tokens, causal, 32 heads of 128, bf16: 622 us with the care for values that are not
 // finite, 884 TFLOP/s of the 1426 that a large product reaches; the matrix pipe works in
 // 48% of the cycles.
+//
+// With heads of 64 the scores are computed where they are needed: four workgroups fit a CU
+// then, not three, and have nothing to do before their first tile (8192 tokens, 16 heads:
+// window 1024 64 us, with the next tile's ahead 74; no window 195 and 191).
 #include <algorithm>
 
 #include "attention.hpp"
@@ -145,8 +149,10 @@ __device__ __forceinline__ void clear_outside(T* out, int64_t token, const int32
 __host__ __device__ inline int64_t o_floats(const ue5m3_attention_t& a) { return a.q_tokens * a.q_heads * a.dim; }
 
 template <typename T, int DT>
-__global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attention_t a, int items, int parts, float* scratch) {
+__global__ __launch_bounds__(kAttnThreads, DT == 64 ? 4 : 2) void attention_kernel(ue5m3_attention_t a, int items, int parts,
+                                                                                  float* scratch) {
     constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
+    constexpr bool AHEAD = DT == 128;
     __shared__ __attribute__((aligned(16))) uint8_t sK[2 * kTile];
     __shared__ __attribute__((aligned(16))) uint8_t sV[2 * kTile];
     __shared__ uint32_t sSpoilt[2][2];               // keys of a tile whose values are not all finite
@@ -239,7 +245,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
             if ((keys & seen) != 0) sum = __builtin_nanf("");
         }
     };
-    // One tile: its scores are there, and the next one's are computed between its
+    // One tile: with AHEAD its scores are there, and the next one's are computed between its
     // exponentials.  The buffer is known when this is compiled, so that the addresses of
     // all reads are a few registers and constants.
     int i = i0;
@@ -249,17 +255,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
         barrier();
         const int j0 = tiles[i] * kKeys;
         ++i;
-        if (i + 1 < i1) issue_k(tiles[i + 1], B);
+        if (AHEAD && i + 1 < i1) issue_k(tiles[i + 1], B);
+        if (!AHEAD && i < i1) issue_k(tiles[i], B ^ 1);
         if (i < i1) issue_v(tiles[i], B ^ 1);
-        const uint8_t *tk = sK + (B ^ 1) * kTile, *tv = sV + B * kTile;
+        const uint8_t *tk = sK + (AHEAD ? B ^ 1 : B) * kTile, *tv = sV + B * kTile;
         if (threadIdx.x < 2) sSpoilt[B ^ 1][threadIdx.x] = 0;       // (of the last turn: all waves have read it)
         if (!ours.all(j0)) clean(sV + B * kTile, sSpoilt[B], j0);
         f32x16 ahead[2];
-        clear(ahead);
+        if (AHEAD) clear(ahead);
         if (mine.none(j0)) {
+            if (!AHEAD) return;
 #pragma unroll
             for (int x = 0; x < kS; ++x) score(tk, x, ahead);
         } else {
+            if (!AHEAD) {
+                clear(s);
+#pragma unroll
+                for (int x = 0; x < kS; ++x) score(tk, x, s);
+            }
             if (!mine.all(j0)) {
                 const int end = last - j0 - 4 * h, start = before - j0 - 4 * h, sinks = sees.sinks - j0 - 4 * h;
 #pragma unroll
@@ -293,41 +306,48 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_kernel(ue5m3_attent
                     sum += u + v;
                     pt[x][y] = pack2<T>(u, v);
                 }
+                if (AHEAD) {
 #pragma unroll
-                for (int z = 0; z < kS / 4; ++z) score(tk, x * (kS / 4) + z, ahead);
+                    for (int z = 0; z < kS / 4; ++z) score(tk, x * (kS / 4) + z, ahead);
+                }
             }
 #pragma unroll
             for (int x = 0; x < 4; ++x)
 #pragma unroll
                 for (int b = 0; b < kB; ++b) o[b] = product32<T>(read_across<DT>(tv, 16 * x, b, lane), pt[x], o[b]);
-            // products and exponentials in turn, operands read ahead of both
-            __builtin_amdgcn_sched_group_barrier(kSgDsRead, 4, 0);
+            if (AHEAD) {                             // products and exponentials in turn, operands read ahead of both
+                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 4, 0);
 #pragma unroll
-            for (int x = 0; x < 2 * kS; ++x) {
-                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgValu, 80 / (2 * kS), 0);
-                __builtin_amdgcn_sched_group_barrier(kSgTrans, 32 / (2 * kS), 0);
-            }
+                for (int x = 0; x < 2 * kS; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kSgDsRead, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kSgValu, 80 / (2 * kS), 0);
+                    __builtin_amdgcn_sched_group_barrier(kSgTrans, 32 / (2 * kS), 0);
+                }
 #pragma unroll
-            for (int x = 0; x < 4 * kB; ++x) {
-                __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+                for (int x = 0; x < 4 * kB; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(kSgMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kSgDsRead, 2, 0);
+                }
             }
         }
+        if (AHEAD) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) s[b] = ahead[b];
+            for (int b = 0; b < 2; ++b) s[b] = ahead[b];
+        }
     };
     if (threadIdx.x < 4) sSpoilt[threadIdx.x / 2][threadIdx.x % 2] = 0;
     if (i0 < i1) {
         issue_k(tiles[i0], 0);
         issue_v(tiles[i0], 0);
-        if (i0 + 1 < i1) issue_k(tiles[i0 + 1], 1);
-        wait_loads<0>();
-        barrier();
-        clear(s);
+        if (AHEAD) {
+            if (i0 + 1 < i1) issue_k(tiles[i0 + 1], 1);
+            wait_loads<0>();
+            barrier();
+            clear(s);
 #pragma unroll
-        for (int x = 0; x < kS; ++x) score(sK, x, s);
+            for (int x = 0; x < kS; ++x) score(sK, x, s);
+        }
     }
     while (i < i1) {
         turn(std::integral_constant<int, 0>{});
