@@ -93,7 +93,10 @@ class Sequence:
         u = U[self.dtype]
         # (a row's largest exponential is 1 at least where P is rounded, so that relative
         # to their sum a step is one at most)
-        return ((u + self.rel) * (self.p @ self.v.abs()) + STEP[self.dtype] / 2 * self.v.abs().sum(1, keepdim=True)
+        # (P is divided by the sum of its rounded values: with P rounded by factors 1 + d,
+        # |d| <= u, o is off by sum(d P (v - o)) / (1 + sum(d P)), at most u / (1 - u)
+        # sum(P |v - o|) <= u / (1 - u) (sum(P |v|) + |o|))
+        return ((u / (1 - u) + self.rel) * (self.p @ self.v.abs() + self.o.abs()) + STEP[self.dtype] / 2 * self.v.abs().sum(1, keepdim=True)
                 + rounding(self.o, self.dtype) + 1e-30)
 
     def gradients(self, do):

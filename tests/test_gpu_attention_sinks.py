@@ -69,3 +69,17 @@ def test_many_sequences():
     """Tiles enough that the rest is in one part."""
     lens = [700] + [20 + i % 7 for i in range(62)] + [90]
     check(lens, lens, 16, 16, 64, 16, 4)
+
+
+def test_one_key_is_exact():
+    """A row that sees one key gives its value, and dS, dQ and dK of it are zeros: dP and
+    do . o are the same sum, but for the order (2 D steps of binary32 of its terms)."""
+    say("one key")
+    for D in (64, 128):
+        q, k, v, do = (rand(i, 200, 2, D).requires_grad_(i < 4) for i in range(1, 5))
+        o = attention(q, k, v, window=1)
+        assert torch.equal(o, v)
+        dq, dk, dv = torch.autograd.grad(o, (q, k, v), do)
+        assert torch.equal(dv, do)
+        ds = 2 * 2 * D * 2.0 ** -24 * (do * v).double().abs().sum(-1, keepdim=True) * D ** -0.5
+        assert (dq.double().abs() <= 1.01 * ds * k.double().abs()).all() and (dk.double().abs() <= 1.01 * ds * q.double().abs()).all()
