@@ -730,8 +730,8 @@ ue5m3_status_t ue5m3_copy_pages(void* base, int64_t planes, int64_t plane, int64
  *     o = sum over seen j of exp(s_j) v_j / sum of exp(s_j), s_j = scale (q . k_j),
  * for q_heads query heads in groups of q_heads / kv_heads, one for each key-value
  * head.  A query that sees nothing gives zeros.  Scores, sums and o are binary32; P
- * (and, of the gradient, dS) is rounded to `type` (bf16 or fp16) for its product; o is
- * rounded once.  What a query does not see does not reach its row, whatever it is; a
+ * (and, of the gradient, dS) is rounded to `type` (bf16 or fp16) for its product, which is
+ * divided by the sum of the rounded P (lse is that of the unrounded ones); o is rounded once.  What a query does not see does not reach its row, whatever it is; a
  * value that it sees and that is not finite makes elements of its row infinite or NaN, or
  * all of it NaN.  lse [q_heads][q_tokens] (nullable) receives log(sum
  * of exp(s_j)), -inf for a query that sees nothing; o_rest (nullable, as o) what the
