@@ -740,8 +740,9 @@ ue5m3_status_t ue5m3_copy_pages(void* base, int64_t planes, int64_t plane, int64
  * bytes (null where that is 0).  q, k and v have strides, o is dense
  * [q_tokens][q_heads][dim].
  *
- * q, k, v, o and o_rest are 16-byte aligned, strides are multiples of 8 elements, dim is a
- * multiple of 8 up to 128.  EINVAL: a type that is not bf16 or fp16, a scale that is
+ * q, k, v, o and o_rest are 16-byte aligned, strides are multiples of 8 elements (that of a
+ * single token or head, which reaches nothing, may be any number), dim is a multiple of 8 up
+ * to 128.  EINVAL: a type that is not bf16 or fp16, a scale that is
  * not positive and finite, causal == 0 with a window, a null pointer; ESHAPE: a
  * negative size, q_heads no multiple of kv_heads, sequences < 1, tokens above 2^30 or no
  * multiple of `sequences` where q_starts is null, a token stride of 2^23 or more or below

@@ -47,11 +47,14 @@ ue5m3_status_t rope_pointers(const ue5m3_rope_t* a) {
     return UE5M3_OK;
 }
 
+// The stride of n things: of one it reaches nothing and may be any number.
+inline int64_t used(int64_t stride, int64_t n) { return n > 1 ? stride : 0; }
+
 // A cache of 16-bit or 32-bit elements, `multiple` of which its strides are multiples of.
-ue5m3_status_t cache_args(const ue5m3_pages_t* c, int64_t multiple) {
+ue5m3_status_t cache_args(const ue5m3_pages_t* c, int32_t heads, int64_t multiple) {
     if (c == nullptr || !power_of_two(c->page_size)) return UE5M3_EINVAL;
     if (c->pages < 0 || c->pages > kMaxPages) return UE5M3_ESHAPE;
-    if (c->page % multiple != 0 || c->token % multiple != 0 || c->head % multiple != 0) return UE5M3_EALIGN;
+    if ((used(c->page, c->pages) | used(c->token, c->page_size) | used(c->head, heads)) % multiple != 0) return UE5M3_EALIGN;
     return UE5M3_OK;
 }
 
@@ -93,7 +96,8 @@ ue5m3_status_t attention_args(const ue5m3_attention_t* a) {
     if (a->k_tokens > 0 && (a->k == nullptr || a->v == nullptr)) return UE5M3_EINVAL;
     if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->o, 16) || !aligned(a->o_rest, 16) || !aligned(a->lse, 4) ||
         !aligned(a->q_starts, 4) || !aligned(a->k_starts, 4) ||
-        (a->q_token | a->q_head | a->k_token | a->k_head | a->v_token | a->v_head) % 8 != 0)
+        (used(a->q_token, a->q_tokens) | used(a->q_head, a->q_heads) | used(a->k_token, a->k_tokens) |
+         used(a->k_head, a->kv_heads) | used(a->v_token, a->k_tokens) | used(a->v_head, a->kv_heads)) % 8 != 0)
         return UE5M3_EALIGN;
     return UE5M3_OK;
 }
@@ -147,7 +151,7 @@ ue5m3_status_t ue5m3_qk_norm_rope_append(const ue5m3_rope_t* args, const void* v
                                          const ue5m3_pages_t* cache, const int64_t* slots, hipStream_t stream) {
     ue5m3_status_t st = rope_args(args, true);
     if (st != UE5M3_OK) return st;
-    if ((st = cache_args(cache, 1)) != UE5M3_OK) return st;
+    if ((st = cache_args(cache, args->kv_heads, 1)) != UE5M3_OK) return st;
     if (args->kv_heads < 1) return UE5M3_ESHAPE;
     if (args->tokens == 0) return UE5M3_OK;
     if ((st = rope_pointers(args)) != UE5M3_OK) return st;
@@ -229,7 +233,7 @@ ue5m3_status_t ue5m3_paged_attention(const ue5m3_paged_attention_t* args, void* 
     const ue5m3_paged_attention_t& a = *args;
     ue5m3_status_t st = head_args(a.type, a.q_heads, a.kv_heads, a.dim, a.scale, a.window, a.sinks);
     if (st != UE5M3_OK) return st;
-    if ((st = cache_args(&a.cache, 8)) != UE5M3_OK) return st;
+    if ((st = cache_args(&a.cache, a.kv_heads, 8)) != UE5M3_OK) return st;
     if (a.rows < 0 || a.rows > kMaxTokens || a.width < 0 || a.width > kMaxTokens / a.cache.page_size ||
         (a.rows > 1 && a.table_row < a.width) || (a.rows > 0 && a.width > 0 && a.cache.pages < 1))
         return UE5M3_ESHAPE;
@@ -242,7 +246,8 @@ ue5m3_status_t ue5m3_paged_attention(const ue5m3_paged_attention_t* args, void* 
         (a.width > 0 && (a.table == nullptr || a.cache.k == nullptr || a.cache.v == nullptr)))
         return UE5M3_EINVAL;
     if (!aligned(a.q, 16) || !aligned(a.o, 16) || !aligned(a.cache.k, 16) || !aligned(a.cache.v, 16) ||
-        !aligned(a.table, 4) || !aligned(a.lengths, 4) || !aligned(scratch, 16) || (a.q_token | a.q_head) % 8 != 0)
+        !aligned(a.table, 4) || !aligned(a.lengths, 4) || !aligned(scratch, 16) ||
+        (used(a.q_token, a.rows) | used(a.q_head, a.q_heads)) % 8 != 0)
         return UE5M3_EALIGN;
     return status(ue5m3::launch_paged_attention(a, (float*)scratch, stream));
 }

@@ -77,7 +77,8 @@ def _on_device(t, name):
 @functools.lru_cache(maxsize=4096)
 def _row_layout(shape, stride, dense):
     """(tokens, token stride, head stride) of [..., heads, dim], None where a copy is
-    needed for them."""
+    needed for them.  Of one token, or one head, the stride reaches nothing and may be any
+    number: 0 then."""
     ok = stride[-1] == 1 or shape[-1] == 1
     token, tokens = stride[-3], _numel(shape[:-2])
     for d in range(len(shape) - 4, -1, -1):              # leading dimensions as one
@@ -86,10 +87,11 @@ def _row_layout(shape, stride, dense):
             ok = ok and (inner <= 1 or stride[d] == token * inner)
             if inner <= 1:
                 token = stride[d]
+    token, head = token if tokens > 1 else 0, stride[-2] if shape[-2] > 1 else 0
     if dense:
-        ok = (ok and (tokens <= 1 or shape[-1] <= token < 1 << 23) and (shape[-2] <= 1 or stride[-2] >= shape[-1])
-              and token % 8 == 0 and stride[-2] % 8 == 0)
-    return (tokens, token, stride[-2]) if ok else None
+        ok = (ok and (tokens <= 1 or shape[-1] <= token < 1 << 23) and (shape[-2] <= 1 or head >= shape[-1])
+              and token % 8 == 0 and head % 8 == 0)
+    return (tokens, token, head) if ok else None
 
 
 def head_rows(t, name, dtypes=_TYPES, dense=False):
@@ -102,7 +104,7 @@ def head_rows(t, name, dtypes=_TYPES, dense=False):
         raise ValueError(f"{name} must be [..., tokens, heads, dim] of " + ", ".join(str(d) for d in dtypes))
     layout = _row_layout(shape, t.stride(), dense)
     if layout is None or dense and t.data_ptr() % 16:
-        t = t.clone() if t.is_contiguous() else t.contiguous()       # (a contiguous one is not aligned)
+        t = dense_like(t).copy_(t)                   # (a clone of a contiguous tensor would keep its strides)
         layout = _row_layout(shape, t.stride(), False)
     return (t, *layout)
 
@@ -246,9 +248,10 @@ def _page_layout(shape, stride, multiple):
     size = shape[1]
     if size < 1 or size & (size - 1):
         raise ValueError("pages hold a power of two of tokens")
-    if any(s % multiple for s in stride[:3]):
+    strides = [s if n > 1 else 0 for n, s in zip(shape[:3], stride)]     # (of one page, token or head: it reaches nothing)
+    if any(s % multiple for s in strides):
         raise ValueError(f"the cache's strides must be multiples of {multiple} elements")
-    return (shape[0], size, *stride[:3])
+    return (shape[0], size, *strides)
 
 
 def cache_arguments(k_cache, v_cache, multiple=1):
@@ -256,10 +259,11 @@ def cache_arguments(k_cache, v_cache, multiple=1):
     _on_device(k_cache, "k_cache")
     _on_device(v_cache, "v_cache")
     shape, stride = k_cache.shape, k_cache.stride()
-    if shape != v_cache.shape or stride != v_cache.stride() or k_cache.dtype != v_cache.dtype:
+    layout = _page_layout(shape, stride, multiple)
+    if (shape != v_cache.shape or k_cache.dtype != v_cache.dtype or
+            stride != v_cache.stride() and layout != _page_layout(shape, v_cache.stride(), multiple)):
         raise ValueError("k_cache and v_cache must have one shape, type and strides")
-    pages, size, page, token, head = _page_layout(shape, stride, multiple)
-    return PagesC(k_cache.data_ptr(), v_cache.data_ptr(), pages, size, page, token, head)
+    return PagesC(k_cache.data_ptr(), v_cache.data_ptr(), *layout)
 
 
 def qk_norm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None, k_weight=None, positions=None, freqs=None,
