@@ -152,16 +152,6 @@ __device__ __forceinline__ void clear_outside(T* out, int64_t token, const int32
 // then their rows' references and sums [parts][heads][tokens][2].
 __host__ __device__ inline int64_t o_floats(const ue5m3_attention_t& a) { return a.q_tokens * a.q_heads * a.dim; }
 
-// The sum of a word's two numbers, and of a third, in binary32.
-template <typename T>
-__device__ __forceinline__ float add_pair(uint32_t w, float c) {
-    typedef std::conditional_t<std::is_same_v<T, bf16>, __bf16, _Float16> T2 __attribute__((ext_vector_type(2)));
-    if constexpr (std::is_same_v<T, bf16>)
-        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(T2, w), T2{1.0f, 1.0f}, c, false);
-    else
-        return __builtin_amdgcn_fdot2(__builtin_bit_cast(T2, w), T2{1.0f, 1.0f}, c, false);
-}
-
 template <typename T, int DT>
 __global__ __launch_bounds__(kAttnThreads, DT == 64 ? 4 : 2) void attention_kernel(ue5m3_attention_t a, int items, int parts,
                                                                                   float* scratch) {

@@ -81,6 +81,16 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
         return make_float2((float)__builtin_bit_cast(f16, (uint16_t)w), (float)__builtin_bit_cast(f16, (uint16_t)(w >> 16)));
 }
 
+// The sum of a word's two numbers, and of a third, in binary32.
+template <typename T>
+__device__ __forceinline__ float add_pair(uint32_t w, float c) {
+    typedef std::conditional_t<std::is_same_v<T, bf16>, __bf16, _Float16> T2 __attribute__((ext_vector_type(2)));
+    if constexpr (std::is_same_v<T, bf16>)
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(T2, w), T2{1.0f, 1.0f}, c, false);
+    else
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(T2, w), T2{1.0f, 1.0f}, c, false);
+}
+
 // 2^x, small results flushed to zero.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

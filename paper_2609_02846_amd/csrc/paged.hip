@@ -7,8 +7,10 @@
 // scores are 16 x 16 x 32 products with the queries as the columns (heads of one
 // key-value head fill them up to 16); keys go from HBM to registers as that
 // product's operand, values to LDS, whence they are read transposed.  Both are
-// loaded a tile ahead, their pages' numbers two.  Parts are joined by a second
-// launch, in their order.
+// loaded a tile ahead, their pages' numbers two.  P is rounded to the queries' type,
+// as the matrix instructions take it, and its product is divided by the sum of the
+// rounded values, as the prompt's attention does it: a row's weights add up to one.  Parts
+// are joined by a second launch, in their order.
 //
 // Bound: HBM, each key and value read once.  One token over 32768 of 8 heads of 128
 // (134 MB): 26.3 us, 5.1 TB/s, what a copy reaches, and 4.7 for the joining; 24 rows of
@@ -180,11 +182,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(ue5m3_p
             const float ref = m == -__builtin_inff() ? 0.0f : m;
             float p[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                p[e] = exp2_fast(s[e / 4][e % 4] - ref);
-                sum += p[e];
-            }
+            for (int e = 0; e < 8; ++e) p[e] = exp2_fast(s[e / 4][e % 4] - ref);
             const u32x4 pt = {pack2<T>(p[0], p[1]), pack2<T>(p[2], p[3]), pack2<T>(p[4], p[5]), pack2<T>(p[6], p[7])};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) sum = add_pair<T>(pt[y], sum);
             // this tile's values are older than the next one's loads
             if (more) wait_loads<kLoads + 2 * kS>();
             else wait_loads<0>();
