@@ -731,9 +731,12 @@ ue5m3_status_t ue5m3_copy_pages(void* base, int64_t planes, int64_t plane, int64
  * for q_heads query heads in groups of q_heads / kv_heads, one for each key-value
  * head.  A query that sees nothing gives zeros.  Scores, sums and o are binary32; P
  * (and, of the gradient, dS) is rounded to `type` (bf16 or fp16) for its product, which is
- * divided by the sum of the rounded P (lse is that of the unrounded ones); o is rounded once.  What a query does not see does not reach its row, whatever it is; a
- * value that it sees and that is not finite makes elements of its row infinite or NaN, or
- * all of it NaN.  lse [q_heads][q_tokens] (nullable) receives log(sum
+ * divided by the sum of the rounded P (lse is that of the unrounded ones); o is rounded once.
+ * What a query does not see does not reach its row, whatever it is.  Of what it sees a value
+ * that is not finite makes elements of its row infinite or NaN, or all of it NaN; a key that
+ * scores -inf weighs nothing, one that scores +inf or NaN makes the row NaN, and so do keys
+ * that all score -inf (of heads of other sizes than 64 and 128 a key with an infinity may
+ * score NaN: they are padded, and 0 times it is added).  lse [q_heads][q_tokens] (nullable) receives log(sum
  * of exp(s_j)), -inf for a query that sees nothing; o_rest (nullable, as o) what the
  * rounding left, rounded to `type` itself: the gradients need more of o than it holds.
  * Tokens of no sequence get zeros (lse -inf).  `scratch` has ue5m3_attention_scratch(args)

@@ -2,7 +2,8 @@
 // it sees times their values, in one pass over the keys with the running maximum
 // and sum.  Query i of a sequence of L queries and S keys stands at position
 // p = i + S - L; it sees key j when j <= p and, under a window, p - j < window or
-// j < sinks.  A row that sees nothing gives zeros.
+// j < sinks.  A row that sees nothing gives zeros; one sees something wherever it has a last
+// key, and where all that it sees scores -inf its softmax is 0 / 0.
 //
 // A workgroup of four waves takes 128 queries of a head, 32 a wave, and walks
 // through the keys 64 at a time.  Scores are computed transposed (keys x
@@ -25,6 +26,7 @@
 // then, not three, and have nothing to do before their first tile (8192 tokens, 16 heads:
 // window 1024 64 us, with the next tile's ahead 74; no window 195 and 191).
 #include <algorithm>
+#include <cfloat>
 
 #include "attention.hpp"
 #include "attn_tile.hpp"
@@ -375,10 +377,11 @@ __global__ __launch_bounds__(kAttnThreads, DT == 64 ? 4 : 2) void attention_kern
                     *(f32x4*)(part_o + (w.q0 + row) * o_token + x) =
                         f32x4{o[b][4 * e] * f, o[b][4 * e + 1] * f, o[b][4 * e + 2] * f, o[b][4 * e + 3] * f};
             }
-        if (h == 0) part_ml[w.q0 + row] = make_float2(m, sum);
+        // (a row whose keys here all score -inf is not one that sees nothing)
+        if (h == 0) part_ml[w.q0 + row] = make_float2(last >= 0 ? fmaxf(m, -FLT_MAX) : m, sum);
         return;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / rounded;
+    const float inv = last < 0 ? 0.0f : 1.0f / rounded;          // (0 / 0 where all seen keys score -inf)
     store_column<T, DT>(o_head + (w.q0 + row) * o_token, o, inv, a.dim);
     if (a.o_rest != nullptr) {
 #pragma unroll
@@ -390,7 +393,8 @@ __global__ __launch_bounds__(kAttnThreads, DT == 64 ? 4 : 2) void attention_kern
     if (lse_head != nullptr && h == 0) lse_head[w.q0 + row] = sum == 0.0f ? -__builtin_inff() : m * kLn2 + logf(sum);
 }
 
-// Outputs from the parts of the keys, in their order; a thread four elements.
+// Outputs from the parts of the keys, in their order; a thread four elements.  Only a row
+// that sees nothing has no reference but -inf.
 template <typename T>
 __global__ __launch_bounds__(kAttnThreads) void attention_join_kernel(ue5m3_attention_t a, int parts, const float* __restrict__ scratch) {
     const int64_t n = o_floats(a), i = ((int64_t)blockIdx.x * kAttnThreads + threadIdx.x) * 4;
@@ -412,7 +416,7 @@ __global__ __launch_bounds__(kAttnThreads) void attention_join_kernel(ue5m3_atte
     const float inv = 1.0f / l;
     u32x2 w, rest;
 #pragma unroll
-    for (int y = 0; y < 4; ++y) v[y] = l == 0.0f ? 0.0f : v[y] * inv;
+    for (int y = 0; y < 4; ++y) v[y] = m == -__builtin_inff() ? 0.0f : v[y] * inv;
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
         w[y] = pack2<T>(v[2 * y], v[2 * y + 1]);

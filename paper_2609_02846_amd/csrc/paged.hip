@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(ue5m3_p
         }
         const int64_t out = row * a.q_heads + kv * group + block * kCols + hc;
         if (parts == 1) {
-            ((T*)a.o)[out * a.dim + d] = (T)(l == 0.0f ? 0.0f : v / l);
+            ((T*)a.o)[out * a.dim + d] = (T)(asked <= 0 ? 0.0f : v / l);     // (0 / 0 where all keys score -inf)
         } else {
             part_o[(out * parts + part) * a.dim + d] = v;
             if (d == 0) part_ml[(out * parts + part) * 2] = top, part_ml[(out * parts + part) * 2 + 1] = l;
@@ -253,6 +253,7 @@ constexpr int kJoinGroups = 8, kJoinThreads = 256;
 template <typename T>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const float* __restrict__ part_o,
                                                                   const float* __restrict__ part_ml, int parts, int dim,
+                                                                  const int32_t* __restrict__ lengths, int q_heads,
                                                                   T* __restrict__ out) {
     __shared__ float so[kJoinGroups][kMaxHead], sl[kJoinGroups], sm[kMaxParts];
     const int64_t at = blockIdx.x;
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const float* _
     float o = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int g = 0; g < kJoinGroups; ++g) o += so[g][e], sum += sl[g];
-    out[at * dim + e] = (T)(sum == 0.0f ? 0.0f : o / sum);
+    out[at * dim + e] = (T)(lengths[at / q_heads] <= 0 ? 0.0f : o / sum);
 }
 
 }  // namespace
@@ -314,7 +315,7 @@ hipError_t launch_paged_attention(const ue5m3_paged_attention_t& a, float* scrat
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && parts > 1) {
             hipLaunchKernelGGL((paged_join_kernel<T>), dim3((unsigned)(a.rows * a.q_heads)), dim3(kJoinThreads), 0, s, scratch,
-                               part_ml, parts, a.dim, (T*)a.o);
+                               part_ml, parts, a.dim, a.lengths, a.q_heads, (T*)a.o);
             e = hipGetLastError();
         }
         return e;
