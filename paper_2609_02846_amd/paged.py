@@ -99,7 +99,8 @@ class PagedCache:
     def extend(self, sequences, counts):
         """Makes room for counts[i] new tokens of each of ``sequences`` (different
         ones); returns their slots, one sequence after the other (int64, on the
-        device).  Raises MemoryError, with nothing changed, where pages lack."""
+        device).  Raises MemoryError where pages lack.  Where it raises, nothing has
+        changed."""
         sequences, counts = list(sequences), [int(c) for c in counts]
         if len(set(sequences)) != len(sequences) or len(counts) != len(sequences) or min(counts, default=0) < 0:
             raise ValueError("each sequence once, with a count that is not negative")
@@ -118,21 +119,35 @@ class PagedCache:
             need += new + (shared is not None)
         if need > len(self._free):
             raise MemoryError(f"{need} pages needed, {len(self._free)} free")
-        src, dst, slots = [], [], []
+        # what can fail comes first, with pages that are free as yet (the last one is taken first)
+        kept = len(self._free) - need
+        free = reversed(self._free[kept:])
+        src, dst, slots, tails = [], [], [], []
         for s, c, shared, new in plan:
-            pages, length = entry = self._sequences[s]
+            pages, length = self._sequences[s]
+            at = length // size                      # what changes: the pages from here on
+            tail = pages[at:]
             if shared is not None:
-                page = self._take()
+                tail[0] = next(free)
                 src.append(shared)
-                dst.append(page)
-                self._uses[shared] -= 1
-                pages[length // size] = page
-            pages.extend(self._take() for _ in range(new))
-            entry[1] = length + c
-            slots.extend(pages[t // size] * size + t % size for t in range(length, length + c))
+                dst.append(tail[0])
+            if new > 0:
+                tail += [next(free) for _ in range(new)]
+            tails.append((at, tail))
+            slots += [tail[t // size - at] * size + t % size for t in range(length, length + c)]
         if src:
             copy_pages(self.storage, src, dst, dim=2)
-        return torch.tensor(slots, dtype=torch.int64, device=self.storage.device)
+        slots = torch.tensor(slots, dtype=torch.int64, device=self.storage.device)
+        for p in self._free[kept:]:
+            self._uses[p] = 1
+        del self._free[kept:]
+        for p in src:
+            self._uses[p] -= 1
+        for (s, c, _, _), (at, tail) in zip(plan, tails):
+            entry = self._sequences[s]
+            entry[0][at:] = tail
+            entry[1] += c
+        return slots
 
     def tables(self, sequences):
         """(table, lengths) of ``sequences`` for ``paged_attention`` (int32, on the
@@ -158,8 +173,3 @@ class PagedCache:
             entry[0] = [to.get(p, p) for p in entry[0]]
         self._free = list(range(used, self.pages))[::-1]
         return used
-
-    def _take(self):
-        p = self._free.pop()
-        self._uses[p] = 1
-        return p
