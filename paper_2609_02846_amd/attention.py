@@ -21,6 +21,12 @@ def _starts(t, name):
     return t
 
 
+def _span(n):
+    """A window or a number of sinks: what passes every length stands for that (as an int64
+    it would come round)."""
+    return min(int(n), 1 << 62)
+
+
 def _heads(q_heads, kv_heads, dim, window, sinks):
     if q_heads < 1 or kv_heads < 1 or q_heads % kv_heads:
         raise ValueError(f"{q_heads} query heads cannot share {kv_heads} key-value heads evenly")
@@ -54,7 +60,7 @@ def _arguments(q, k, v, q_starts, k_starts, scale, causal, window, sinks):
         if k_starts.numel() != q_starts.numel():
             raise ValueError("q_starts and k_starts must name the same number of sequences")
         sequences = q_starts.numel() - 1
-    window, sinks = int(window), int(sinks)
+    window, sinks = _span(window), _span(sinks)
     _heads(q.shape[-2], k.shape[-2], q.shape[-1], window, sinks)
     if window and not causal:
         raise ValueError("a window belongs to causal attention")
@@ -158,7 +164,7 @@ def paged_attention(q, k_cache, v_cache, table, lengths, scale=None, window=0, s
     if table.stride(1) != 1 and table.shape[1] > 1 or rows > 1 and table.stride(0) < table.shape[1]:
         table = table.contiguous()
     lengths = lengths.contiguous()
-    width, window, sinks = table.shape[1], int(window), int(sinks)
+    width, window, sinks = table.shape[1], _span(window), _span(sinks)
     _heads(q.shape[1], k_cache.shape[2], q.shape[2], window, sinks)
     lib = load_library()
     o = dense_like(q)

@@ -919,7 +919,8 @@ int far_parts_of(const ue5m3_attention_t& a, int parts) {
 
 int64_t attention_grad_scratch(const ue5m3_attention_t& a) {
     const int parts = dkv_parts_of(a), far = far_parts_of(a, parts);
-    return (delta_floats(a) + (parts > 1 || far > 0 ? 2 * parts * dkv_floats(a) + 2 * far * far_floats(a) : 0)) * 4;
+    const int64_t sinks = far > 0 ? 2 * far * far_floats(a) : 0;     // (any number of sinks may be asked for where there are none)
+    return (delta_floats(a) + (parts > 1 || far > 0 ? 2 * parts * dkv_floats(a) + sinks : 0)) * 4;
 }
 
 hipError_t launch_attention_grad(const ue5m3_attention_t& a, const ue5m3_attention_grad_t& g, hipStream_t s) {
