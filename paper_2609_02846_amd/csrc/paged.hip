@@ -91,9 +91,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(ue5m3_p
     const uint16_t* const v_head = (const uint16_t*)a.cache.v + kv * a.cache.head;
     // Element offset of key j's row, whose page's number is n; a number outside the
     // cache is noted, and page 0 read.
-    auto offset = [&](int j, int n, bool counts) {
+    auto offset = [&](int j, int n) {
         const bool ok = (uint32_t)n < (uint64_t)a.cache.pages;
-        bad |= counts && !ok;
+        bad |= !ok;
         return (int64_t)(ok ? n : 0) * a.cache.page + (int64_t)(j & mask) * a.cache.token;
     };
     // Keys of a tile that a lane needs: two for its operand of the scores, kLoads for
@@ -122,12 +122,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(ue5m3_p
         for (int i = 0; i < kLoads; ++i) {
             const int r = value_row(i), c = lane % kChunks ^ value_swizzle<DT>(r);
             const int key = key_at(j, end, r);
-            load_16(v_head + offset(key, n.v[i], true) + (8 * c < a.dim ? 8 * c : 0), lds + buffer * kTile + i * 1024);
+            load_16(v_head + offset(key, n.v[i]) + (8 * c < a.dim ? 8 * c : 0), lds + buffer * kTile + i * 1024);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int key = key_at(j, end, 16 * i + col);
-            const uint16_t* p = k_head + offset(key, n.k[i], true);
+            const uint16_t* p = k_head + offset(key, n.k[i]);
 #pragma unroll
             for (int s = 0; s < kS; ++s) __builtin_memcpy(&to[i][s], p + (32 * s + 8 * g < a.dim ? 32 * s + 8 * g : 0), 16);
         }

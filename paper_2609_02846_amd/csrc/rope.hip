@@ -11,8 +11,8 @@
 //     dx = r (g w - x r^2 mean(g w x)),  dw = sum over rows of g x r.
 // All in binary32, rounded once; the angle in binary64, since far positions
 // times the first frequencies are thousands of turns: in quarter turns, less the
-// nearest whole number of them, it is rounded to binary32 with an error of 2^-27
-// of a quarter turn.
+// nearest whole number of them, it is at most 1/2 and rounded to binary32 with an
+// error of up to 2^-26 of a quarter turn.
 #include <algorithm>
 #include <cmath>
 
