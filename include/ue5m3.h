@@ -730,8 +730,8 @@ ue5m3_status_t ue5m3_copy_pages(void* base, int64_t planes, int64_t plane, int64
  *     o = sum over seen j of exp(s_j) v_j / sum of exp(s_j), s_j = scale (q . k_j),
  * for q_heads query heads in groups of q_heads / kv_heads, one for each key-value
  * head.  A query that sees nothing gives zeros.  Scores, sums and o are binary32; P
- * (and, of the gradient, dS) is rounded to `type` (bf16 or fp16) for its product, which is
- * divided by the sum of the rounded P (lse is that of the unrounded ones); o is rounded once.
+ * is rounded to `type` (bf16 or fp16) for its product, which is divided by the sum of the
+ * rounded P (lse is that of the unrounded ones); o is rounded once.
  * What a query does not see does not reach its row, whatever it is.  Of what it sees a value
  * that is not finite makes elements of its row infinite or NaN, or all of it NaN; a key that
  * scores -inf weighs nothing, one that scores +inf or NaN makes the row NaN, and so do keys
@@ -772,7 +772,8 @@ ue5m3_status_t ue5m3_attention(const ue5m3_attention_t* args, void* scratch, hip
  * Its gradients for the output gradient d_o (dense): with P = exp(s - lse) and
  * delta = sum(d_o (o + o_rest)) of each row, dS = P (d_o . v - delta), dq = scale dS k,
  * dk = scale dS^T q, dv = P^T d_o, the last two summed over the query heads that share
- * a key-value head, in a fixed order.  `args` as of the forward call, with its o,
+ * a key-value head, in a fixed order.  P is rounded to `type` for dv's product, dS goes to its
+ * two as two numbers of it, its rounding and that of the rest.  `args` as of the forward call, with its o,
  * o_rest and lse; `scratch` has ue5m3_attention_grad_scratch(args) bytes.  dq, or dk and dv
  * together, may be null.  16-byte alignment and strides as for q, k and v.  EINVAL also: a
  * type that is not bf16 (of fp16, dS of a mean over tokens is below the normal numbers).

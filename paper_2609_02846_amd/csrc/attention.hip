@@ -428,14 +428,27 @@ __global__ __launch_bounds__(kAttnThreads) void attention_join_kernel(ue5m3_atte
     if (a.lse != nullptr && d == 0) a.lse[head * a.q_tokens + token] = l == 0.0f ? -__builtin_inff() : m * kLn2 + logf(l);
 }
 
+// Half x of a lane's 16 values, each as two numbers of the type: its rounding, and the
+// rounding of what that left.
+template <typename T>
+__device__ __forceinline__ void two_numbers(const f32x16& s, int x, u32x4& first, u32x4& rest) {
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        const float u = s[8 * x + 2 * y], v = s[8 * x + 2 * y + 1];
+        first[y] = pack2<T>(u, v);
+        const float2 r = unpack2<T>(first[y]);
+        rest[y] = pack2<T>(u - r.x, v - r.y);
+    }
+}
+
 // dQ, and the rows' sums do . o, which both halves of the backward pass take.
 // As the forward kernel; P is exp(score - lse) and dS = P (dP - do . o) goes to its
 // product as two numbers of the inputs' type, its rounding and the rounding of what that
 // left (one product more for each operand read: 730 us against 916, 8% of a training
 // step).  dP and do . o often nearly cancel, so the rounding of o would be the largest
 // error of dS: the forward pass keeps what it left, too.  In relative L2 norm dQ and dK of
-// 8192 tokens are 1.9e-3 and 2.4e-3 from the exact ones, 1.7e-3 of which their own rounding
-// makes; with dS in one number dQ is 2.6e-3 off, with o as it was rounded 3.4e-3.
+// 8192 tokens are 1.7e-3 from the exact ones, which is their own rounding; with dS in one
+// number dQ is 2.6e-3 off and dK 2.4e-3, with o as it was rounded dQ 3.4e-3.
 //
 // Bound: the products.  8192 tokens, 32 heads of 128: 916 us for 0.82 TF, 1.10 with the
 // second number, 1200 TFLOP/s; the matrix pipe works in 62% of the cycles.
@@ -535,13 +548,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_att
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 u32x4 ds, rest;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const float u = s[8 * x + 2 * y], v = s[8 * x + 2 * y + 1];
-                    ds[y] = pack2<T>(u, v);
-                    const float2 r = unpack2<T>(ds[y]);
-                    rest[y] = pack2<T>(u - r.x, v - r.y);
-                }
+                two_numbers<T>(s, x, ds, rest);
 #pragma unroll
                 for (int y = 0; y < kB; ++y) {
                     const u32x4 f = read_across<DT>(tk, 32 * b + 16 * x, y, lane);
@@ -575,7 +582,9 @@ __host__ __device__ inline int64_t far_floats(const ue5m3_attention_t& a) { retu
 // it in turn: the sum over those heads is made here, in a fixed order.
 //
 // Scores are queries x keys here, so that P and dS are the operands of the products that
-// contract over queries.  A wave's keys stay in registers, its values in LDS: with both in
+// contract over queries.  P goes to dV's in one number (dV is 2.3e-3 off, 1.7e-3 of which its
+// own rounding makes), dS to dK's in two, as for dQ (a fifth product, for operands that are
+// read anyway: a training step of 8192 tokens 2660 us without, 2840 with it).  A wave's keys stay in registers, its values in LDS: with both in
 // registers there would be room for one wave a SIMD only, and nothing to fill its waits
 // (8192 tokens, 32 heads of 128, 8 of keys: 1730 us against 1230).
 //
@@ -759,11 +768,14 @@ __global__ __launch_bounds__(kAttnThreads, DT == 64 ? 3 : 2) void attention_dkv_
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            u32x4 ds;
+            u32x4 ds, rest;
+            two_numbers<T>(s, x, ds, rest);
 #pragma unroll
-            for (int y = 0; y < 4; ++y) ds[y] = pack2<T>(s[8 * x + 2 * y], s[8 * x + 2 * y + 1]);
-#pragma unroll
-            for (int y = 0; y < kB; ++y) dk[y] = product32<T>(read_across<DT>(tq, 16 * x, y, lane), ds, dk[y]);
+            for (int y = 0; y < kB; ++y) {
+                const u32x4 f = read_across<DT>(tq, 16 * x, y, lane);
+                dk[y] = product32<T>(f, ds, dk[y]);
+                dk[y] = product32<T>(f, rest, dk[y]);
+            }
         }
     };
     auto turn = [&](auto buffer) __attribute__((always_inline)) {
