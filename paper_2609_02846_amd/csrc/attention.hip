@@ -17,10 +17,14 @@
 // before the rounding goes to lse.  Scores, sums and the output are binary32.
 //
 // Bound: the two products and, in their shadow, the exponentials: the scores of the next
-// tile are computed between this one's (8192 tokens 594 us, one after the other 639).
-// 8192 tokens, causal, 32 heads of 128, bf16: 655 us with the care for values that are not
-// finite and both sums, 840 TFLOP/s of the 1426 that a large product reaches; the matrix pipe works in
-// 48% of the cycles.
+// tile are computed between this one's (before values that are not finite were cared for and
+// the second sum was kept, 8192 tokens 594 us, one after the other 639, in one run).
+// 8192 tokens, causal, 32 heads of 128, bf16: 580 us in a warm run, 600 to 655 in the first
+// passes of a process; 950 TFLOP/s of the 1443 that a large product reaches.  The matrix pipe
+// works in 41% of the cycles, LDS in 22%; 40% of a wave's go by at waits (a tile's loads and
+// its barrier), 23% at instructions that others' take the place of.  Not causal: 1100 us, 1000
+// TFLOP/s.  Heads of other sizes take the products of 64 or 128: 96 561 us, 80 535, of 64 330,
+// 32 313.
 //
 // With heads of 64 the scores are computed where they are needed: four workgroups fit a CU
 // then, not three, and have nothing to do before their first tile (8192 tokens, 16 heads:
@@ -450,8 +454,8 @@ __device__ __forceinline__ void two_numbers(const f32x16& s, int x, u32x4& first
 // 8192 tokens are 1.7e-3 from the exact ones, which is their own rounding; with dS in one
 // number dQ is 2.6e-3 off and dK 2.4e-3, with o as it was rounded dQ 3.4e-3.
 //
-// Bound: the products.  8192 tokens, 32 heads of 128: 916 us for 0.82 TF, 1.10 with the
-// second number, 1200 TFLOP/s; the matrix pipe works in 62% of the cycles.
+// Bound: the products.  8192 tokens, 32 heads of 128: 900 us for 0.82 TF, 1.10 with the
+// second number, 1220 TFLOP/s; the matrix pipe works in 63% of the cycles, LDS in 24%.
 template <typename T, int DT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attention_dq_kernel(ue5m3_attention_t a, ue5m3_attention_grad_t g, int items) {
     constexpr int kTile = kKeys * DT * 2, kB = DT / 32, kS = DT / 16;
@@ -586,14 +590,15 @@ __host__ __device__ inline int64_t far_floats(const ue5m3_attention_t& a) { retu
 // own rounding makes), dS to dK's in two, as for dQ (a fifth product, for operands that are
 // read anyway: a training step of 8192 tokens 2660 us without, 2840 with it).  A wave's keys stay in registers, its values in LDS: with both in
 // registers there would be room for one wave a SIMD only, and nothing to fill its waits
-// (8192 tokens, 32 heads of 128, 8 of keys: 1730 us against 1230).
+// (8192 tokens, 32 heads of 128, 8 of keys, dS in one number: 1730 us against 1230).
 //
-// Bound: the products, 4 of 2 pairs x heads x dim operations, and LDS, which holds Q and
-// dO for two reads each: those 1.10 TF take 1230 us (893 TFLOP/s), the matrix pipe works
-// in 43% of the cycles, half of the waves' others go on waiting for reads of LDS.  With heads
-// of 64 three workgroups fit a CU, which is worth more than products ordered between the
-// exponentials by hand, for which there are registers with two only (packed sequences of
-// 8192 tokens, window 1024, 4 sinks: 108 us against 119).
+// Bound: the products, 4 of 2 pairs x heads x dim operations and one more for dS's second
+// number: those 1.37 TF take 1270 us (1080 TFLOP/s).  The matrix pipe works in 49% of the
+// cycles and LDS, which holds Q and dO for two reads each, in 30%; 46% of a wave's go by at
+// waits, for reads of LDS and at the barrier of a tile.  With heads of 64 three workgroups
+// fit a CU, which is worth more than products ordered between the exponentials by hand, for
+// which there are registers with two only (packed sequences of 8192 tokens, window 1024, 4
+// sinks, dS in one number: 108 us against 119; in two 120).
 //
 // Under a window the first tile of a sequence has all rows to visit where the others have
 // the window's: the rows that see its sinks only are cut into `far` parts of their own.
@@ -903,7 +908,8 @@ hipError_t launch_attention(const ue5m3_attention_t& a, float* scratch, hipStrea
 
 // Parts that a key tile's queries are cut into.  Causal tiles differ in length, and two
 // workgroups run on a CU: with four for each CU, the longest first, all CUs end together
-// (8192 tokens, 8 key-value heads: one part 2041 us, two 1241 with their sum).  A part has
+// (8192 tokens, 8 key-value heads, dS in one number: one part 2041 us, two 1241 with their
+// sum).  A part has
 // 16 tiles of queries at least, by the sequences' mean length.
 int dkv_parts_of(const ue5m3_attention_t& a) {
     if (a.q_tokens == 0 || a.k_tokens == 0) return 1;
@@ -916,8 +922,8 @@ int dkv_parts_of(const ue5m3_attention_t& a) {
 // they stay with the others): of the longest that a sequence can be, about as many turns
 // each as a part of the other tiles has, two for each sequence at least, and no more of
 // them than memory for two parts of all keys holds (8192 tokens, window 1024, 4 sinks, 32
-// heads of 128, 8 of keys, forward and gradients: 1550 us with them among the others, 899
-// apart; 16 heads of 64 494 and 303).
+// heads of 128, 8 of keys, forward and gradients, dS of dK in one number: 1550 us with them
+// among the others, 899 apart; 16 heads of 64 494 and 303).
 int far_parts_of(const ue5m3_attention_t& a, int parts) {
     if (!a.causal || a.window == 0 || a.sinks == 0 || a.sinks > kRows || a.sequences * a.kv_heads >= 1 << 21) return 0;
     const int64_t n = a.q_starts != nullptr ? 1 : a.sequences, group = a.q_heads / a.kv_heads;

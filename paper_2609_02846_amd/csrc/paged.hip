@@ -13,8 +13,11 @@
 // are joined by a second launch, in their order.
 //
 // Bound: HBM, each key and value read once.  One token over 32768 of 8 heads of 128
-// (134 MB): 26.3 us, 5.1 TB/s, what a copy reaches, and 4.7 for the joining; 24 rows of
-// up to 8191 (232 MB): 62 us, 3.7 TB/s, as the last rows to end leave CUs idle.
+// (134 MB): 26.4 us, 5.1 TB/s, what a copy reaches, and 5.0 for the joining; 24 rows of
+// up to 8191 (232 MB): 62 us, 3.7 TB/s, as parts are cut by the table's width: the short
+// rows' end early and leave CUs idle (24 rows of 8192: 157 us, 5.1 TB/s).  On a cache that
+// lies in the chip's own one: the 24 rows 54 us, under a window of 1024 with 4 sinks 21 (62
+// MB), with heads of 80 46 (145 MB), of 64 31 (116 MB).
 #include <algorithm>
 
 #include "attention.hpp"

@@ -317,7 +317,10 @@ __global__ __launch_bounds__(kRopeThreads) void rope_grad_kernel(ue5m3_rope_t r,
 
 // ---- any other heads ----
 // A wave for each row of a head: any size, two pairs a lane and up to four of
-// the elements that pass.
+// the elements that pass.  Bound: the angles in binary64, which each row works out for
+// itself, and loads of one element a lane: 8192 tokens of 40 heads of 100, bf16 (131 MB) take
+// 161 us (heads of 128 by lanes of eight, of the same tensors again and again, 34), with
+// gradients 443 (94); heads of 50 as long.
 template <typename T>
 struct Row {
     float a[2], b[2], c[4];
