@@ -586,9 +586,11 @@ __host__ __device__ inline int64_t far_floats(const ue5m3_attention_t& a) { retu
 // it in turn: the sum over those heads is made here, in a fixed order.
 //
 // Scores are queries x keys here, so that P and dS are the operands of the products that
-// contract over queries.  P goes to dV's in one number (dV is 2.3e-3 off, 1.7e-3 of which its
-// own rounding makes), dS to dK's in two, as for dQ (a fifth product, for operands that are
-// read anyway: a training step of 8192 tokens 2660 us without, 2840 with it).  A wave's keys stay in registers, its values in LDS: with both in
+// contract over queries.  P goes to dV's in one number (dV is 2.2e-3 off, 1.7e-3 of which its
+// own rounding makes, and 2.5e-3 at most over sequences of all lengths), dS to dK's in two, as
+// for dQ (in one dK is 2.4e-3 off, of a few tokens up to 3.2e-3, twice its own rounding; it is
+// a fifth product, for operands that are read anyway: a training step of 8192 tokens 2660 us
+// without, 2840 with it).  A wave's keys stay in registers, its values in LDS: with both in
 // registers there would be room for one wave a SIMD only, and nothing to fill its waits
 // (8192 tokens, 32 heads of 128, 8 of keys, dS in one number: 1730 us against 1230).
 //
